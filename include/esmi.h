@@ -367,6 +367,117 @@ es_status es_get_problem_data(es_handle* h, float* out);
 es_status es_debug_noise(es_handle* h, int32_t run, int64_t t, int32_t pair,
                          uint32_t* words, float* eps);
 
+/* ---- Operators of networks -------------------------------------------------
+ *
+ * What a program with a network of its own calls beside the strategies: the
+ * layers of a population's networks (the members es_ask hands out hold their
+ * parameters, Sec. 3.2's parameter reshaping) or of one network (the mean),
+ * their gradients, and an optimiser step outside es_tell.  They need no
+ * handle: every call enqueues kernels on hip_stream, allocates nothing and
+ * keeps nothing from one call to the next; the device of the pointers and of
+ * the stream must be current.  All can be captured into a graph.  Errors are
+ * reported through es_last_error(NULL); a refused call has enqueued nothing.
+ *
+ * Types.  ES_F32, ES_BF16 and ES_F16.  Products of 16-bit operands run on the
+ * matrix cores and all sums are held in fp32; results are rounded to nearest
+ * once, where they are stored. */
+typedef enum { ES_F32 = 0, ES_BF16 = 1, ES_F16 = 2 } es_dtype;
+
+/* Activations a(z): 0, z; 1, max(z, 0); 2, tanh z; 3, z Phi(z) with Phi the
+ * normal distribution function (the erf form of GELU); 4, z / (1 + e^-z). */
+typedef enum { ES_ACT_NONE = 0, ES_ACT_RELU = 1, ES_ACT_TANH = 2, ES_ACT_GELU = 3, ES_ACT_SILU = 4 } es_activation;
+
+/* A matrix per member: element (n, i, j) at p[n*member + i*row + j], strides
+ * in elements.  member 0: the same matrix for all members.  p NULL: absent
+ * (where that is allowed).  Any alignment of the element's size; whole rows
+ * of 16 bytes at multiples of 16 are the fastest. */
+typedef struct es_matrix {
+    void* p;
+    int64_t member, row;
+} es_matrix;
+
+/* dense:  z[n,i,o] = sum_k x[n,i,k] w[n,o,k] + bias[n,o],
+ *         y = act(z) + residual;  pre (if present) receives z.
+ * gated:  w and bias have 2 out rows, gate rows first: with g = the first
+ *         out columns of z and u = the others,
+ *         y = act(g) u;  pre [..][2 out] receives z.  No residual.
+ *   x [members][rows][in], w [members][out or 2 out][in], bias [members][out
+ *   or 2 out] (its row stride is not used; NULL: none), residual and y
+ *   [members][rows][out].
+ * All of the type dtype but y, which has y_dtype: dtype or ES_F32.  y may be
+ * the residual's own memory (same strides and type); no other output may
+ * overlap anything else.  rows, in, out and members may be 0 or 1: a sum of
+ * no terms is 0. */
+typedef struct es_dense_args {
+    int32_t dtype, y_dtype, act, reserved; /* reserved: 0 */
+    int64_t members, rows, in, out;
+    es_matrix x, w, bias, residual, y, pre;
+} es_dense_args;
+
+/* Gradients of the above for dy = dL/dy, given the kept pre (dense without
+ * activation: pre is not used and may be NULL):
+ *   dz = dy act'(pre), or [dy u act'(g), dy act(g)] for gated;
+ *   dx[n,i,k] = sum_o dz[n,i,o] w[n,o,k],  dw[n,o,k] = sum_i dz[n,i,o] x[n,i,k],
+ *   db[n,o] = sum_i dz[n,i,o].  The residual's gradient is dy itself.
+ * dx, dw, db: NULL to skip.  One whose member stride is 0 receives the sum
+ * over the members (the gradient of an operand that they share).  All of the
+ * type dtype; dz is rounded to it before the two products (db sums it
+ * unrounded). */
+typedef struct es_dense_grad_args {
+    int32_t dtype, act;
+    int64_t members, rows, in, out;
+    es_matrix dy, x, w, pre, dx, dw, db;
+} es_dense_grad_args;
+
+/* workspace: device memory of at least the size that the _workspace query of
+ * the same arguments gives (host value, no device work; 0: NULL is taken),
+ * aligned to 256 bytes and used by this call alone until the stream has
+ * passed it. */
+es_status es_dense_workspace(const es_dense_args* a, size_t* bytes);
+es_status es_dense(const es_dense_args* a, void* workspace, size_t bytes, void* hip_stream);
+es_status es_dense_backward_workspace(const es_dense_grad_args* a, size_t* bytes);
+es_status es_dense_backward(const es_dense_grad_args* a, void* workspace, size_t bytes, void* hip_stream);
+es_status es_gated_workspace(const es_dense_args* a, size_t* bytes);
+es_status es_gated(const es_dense_args* a, void* workspace, size_t bytes, void* hip_stream);
+es_status es_gated_backward_workspace(const es_dense_grad_args* a, size_t* bytes);
+es_status es_gated_backward(const es_dense_grad_args* a, void* workspace, size_t bytes, void* hip_stream);
+
+/* AdamW (Loshchilov & Hutter 2019) on many tensors at once, t = step >= 1:
+ *   m <- beta1 m + (1 - beta1) g,  v <- beta2 v + (1 - beta2) g^2,
+ *   q = (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps),
+ *   p <- p (1 - lr weight_decay) - lr q.
+ * With weight_decay 0 and 32-bit states this is es_tell's Adam step bit for
+ * bit (t one more than the generation).
+ * state_bits 32: m and v fp32 [n].
+ * state_bits 8:  m and v hold codes, OCP e4m3 (no infinities), of m and of
+ *   sqrt(v); each block of 256 elements shares an fp32 scale (m_scale,
+ *   v_scale [ceil(n/256)]), the largest finite magnitude / 448 (at least
+ *   2^-126): value = code * scale.  Codes are rounded to nearest; a sqrt(v)
+ *   above 0 never becomes 0; a non-finite value is kept as NaN and leaves its
+ *   neighbours' scale alone.  The step itself uses the moments before they
+ *   are rounded.
+ * p fp32; g of g_dtype; copy (NULL: none) receives p rounded to copy_dtype
+ * (ES_BF16 or ES_F16).  lr and weight_decay are per tensor.  The tensors may
+ * not overlap.  tensors: host array, read before the call returns. */
+typedef struct es_adamw_tensor {
+    float* p;
+    const void* g;
+    void *m, *v;
+    float *m_scale, *v_scale; /* state_bits 8, else NULL */
+    void* copy;
+    int64_t n;
+    float lr, weight_decay;
+} es_adamw_tensor;
+
+typedef struct es_adamw_args {
+    int32_t count, g_dtype, state_bits, copy_dtype;
+    int64_t step;
+    float beta1, beta2, eps;
+    int32_t reserved; /* 0 */
+} es_adamw_args;
+
+es_status es_adamw(const es_adamw_args* a, const es_adamw_tensor* tensors, void* hip_stream);
+
 /* Checkpoint (synchronous; the paper defines none -- the state is that of
  * Listing 1): with host_buf NULL, *bytes receives the size;
  * otherwise the state (config, t, m, m1, v, best, per-run sigma and lr, the
@@ -412,7 +523,8 @@ int32_t es_run_path(const es_handle* h, int32_t* keeps_normals);
 int32_t es_eval_path(const es_config* cfg, int64_t* partial_floats);
 
 /* Message of the last failed call on h ("" if none); with h == NULL, the
- * message of the last failed es_init on this thread.  Never NULL. */
+ * message of the last failed es_init, es_eval_noalloc or operator of networks
+ * on this thread.  Never NULL. */
 const char* es_last_error(const es_handle* h);
 
 /* Static description of a status code. */

@@ -32,13 +32,13 @@ static_assert(sizeof(es_config) == 168, "es_config has padding");
 
 thread_local char g_init_err[256] = {0};
 
-es_status init_fail(es_status s, const char* msg, const char* who = "es_init")
+}  // namespace
+
+es_status esmi::init_fail(es_status s, const char* msg, const char* who)
 {
     std::snprintf(g_init_err, sizeof(g_init_err), "%s: %s", who, msg);
     return s;
 }
-
-}  // namespace
 
 struct es_handle {
     es_config cfg;

@@ -1,0 +1,65 @@
+// es_dense.hpp -- what the layer kernels (es_dense.hip) and their entry points
+// (es_layers.cpp) share.  Not part of the C-ABI.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "esmi.h"
+
+namespace esmi {
+
+constexpr size_t dtype_size(int32_t t) { return t == ES_F32 ? 4 : 2; }
+
+// One matrix product per batch, C[m][n] = sum over r < red and k < K of
+// A(m, k) B(n, k), and what follows it.  An operand is "k-major" where its k
+// index is the contiguous one (x and w of the forward), else its m (n) index
+// is (w of dx; dz and x of dw).
+struct Gemm {
+    int32_t dtype;
+    int32_t M, N, K;
+    int64_t batches, red;
+    const void *a, *b;
+    int64_t a_batch, a_red, a_row;  // element strides; a_row between rows of the memory's matrix
+    int64_t b_batch, b_red, b_row;
+    bool a_kmajor, b_kmajor;
+    // gated: N counts the outputs; B has 2 N rows, the gates' first
+    bool gated;
+    int32_t act;
+    const void* bias;
+    int64_t bias_batch;
+    const void* res;
+    int64_t res_batch, res_row;
+    void* pre;
+    int64_t pre_batch, pre_row;
+    void* c;
+    int64_t c_batch, c_row;
+    int32_t c_dtype;
+};
+
+// Floats of partial sums that the product keeps between its two launches
+// where its reduction is split (0: one launch).
+size_t gemm_workspace_floats(const Gemm& g);
+hipError_t launch_gemm(const Gemm& g, float* partial, hipStream_t s);
+bool gemm_too_large(const Gemm& g);  // more workgroups than a launch holds
+
+// dz = dy act'(pre) (or both halves of a gated layer) in the type, rows of
+// ldz elements, and the column sums of the unrounded dz per chunk of rows.
+struct GradZ {
+    int32_t dtype, act;
+    bool gated;
+    int64_t members;
+    int32_t rows, out;  // out: columns of dy
+    const void *dy, *pre;
+    int64_t dy_member, dy_row, pre_member, pre_row;
+    void* dz;  // null: not stored
+    int64_t ldz;
+    float* sums;  // [members][chunks][wide], null: not wanted
+};
+int64_t gradz_chunks(int64_t rows);
+hipError_t launch_gradz(const GradZ& g, hipStream_t s);
+// db[n][o] (db_member 0: summed over the members) from the chunks' sums
+hipError_t launch_bias_grad(int32_t dtype, const float* sums, int64_t members, int64_t chunks, int64_t wide, void* db,
+                            int64_t db_member, hipStream_t s);
+
+}  // namespace esmi

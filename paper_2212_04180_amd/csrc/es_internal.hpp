@@ -242,4 +242,7 @@ constexpr int32_t POP_MAX_N = 1 << 24;
 // 0.67 33 against 72, 2.7 93 against 98).
 constexpr double RANK_SORT_FROM_WORK = 1.2e8;
 
+// Records the message that es_last_error(NULL) gives on this thread.
+es_status init_fail(es_status s, const char* msg, const char* who = "es_init");
+
 }  // namespace esmi

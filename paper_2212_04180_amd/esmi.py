@@ -29,6 +29,8 @@ EXPORTS = ("es_init", "es_ask", "es_eval", "es_eval_timed", "es_eval_noalloc", "
            "es_get_best", "es_get_shaped", "es_get_grad", "es_set_hparams", "es_get_hparams",
            "es_get_strategy_state", "es_set_strategy_state", "es_get_penalty",
            "es_get_problem_data", "es_debug_noise",
+           "es_dense_workspace", "es_dense", "es_dense_backward_workspace", "es_dense_backward",
+           "es_gated_workspace", "es_gated", "es_gated_backward_workspace", "es_gated_backward", "es_adamw",
            "es_save_state", "es_load_state", "es_sync", "es_generation", "es_run_path", "es_eval_path",
            "es_last_error", "es_status_string", "es_destroy")
 
@@ -176,6 +178,12 @@ def lib() -> ctypes.CDLL:
         "es_set_strategy_state": (i32, [vp, vp, vp]),
         "es_get_problem_data": (i32, [vp, vp]),
         "es_debug_noise": (i32, [vp, i32, i64, i32, vp, vp]),
+        # the operators of networks take their packed argument structs as bytes (operators.py)
+        **{f"es_{op}{way}": (i32, [ctypes.c_char_p, vp, ctypes.c_size_t, vp])
+           for op in ("dense", "gated") for way in ("", "_backward")},
+        **{f"es_{op}{way}_workspace": (i32, [ctypes.c_char_p, P(ctypes.c_size_t)])
+           for op in ("dense", "gated") for way in ("", "_backward")},
+        "es_adamw": (i32, [ctypes.c_char_p, ctypes.c_char_p, vp]),
         "es_save_state": (i32, [vp, vp, P(ctypes.c_size_t)]),
         "es_load_state": (i32, [vp, vp, ctypes.c_size_t]),
         "es_sync": (i32, [vp]),
