@@ -19,57 +19,13 @@
 #include <math.h>
 
 #include "es_dense.hpp"
+#include "es_dense_device.hpp"
 
 namespace esmi {
 
 namespace {
 
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-typedef float floatx4 __attribute__((ext_vector_type(4)));
-typedef uint32_t uintx4 __attribute__((ext_vector_type(4)));
-
-// ---- activations, fp32 ----------------------------------------------------
-__device__ __forceinline__ float act_value(float z, int32_t act)
-{
-    switch (act) {
-    case ES_ACT_RELU: return z <= 0.f ? 0.f : z;  // NaN stays
-    case ES_ACT_TANH: return tanhf(z);
-    case ES_ACT_GELU: return 0.5f * z * erfcf(-0.70710678118654752440f * z);
-    case ES_ACT_SILU: return z / (1.f + expf(-z));
-    default: return z;
-    }
-}
-
-__device__ __forceinline__ float act_slope(float z, int32_t act)
-{
-    switch (act) {
-    case ES_ACT_RELU: return z > 0.f ? 1.f : z != z ? z : 0.f;
-    case ES_ACT_TANH: {
-        const float t = tanhf(z);
-        return (1.f - t) * (1.f + t);
-    }
-    case ES_ACT_GELU:
-        return 0.5f * erfcf(-0.70710678118654752440f * z) + z * expf(-0.5f * z * z) * 0.39894228040143267794f;
-    case ES_ACT_SILU: {
-        const float s = 1.f / (1.f + expf(-z));
-        return s * (1.f + z * (1.f - s));
-    }
-    default: return 1.f;
-    }
-}
-
-template <typename T>
-__device__ __forceinline__ float widen(T v) { return (float)v; }
-
 // ---- the product ----------------------------------------------------------
-struct GemmArgs {
-    Gemm g;
-    int32_t splits;        // of the reduction; 1: C is finished here
-    int32_t mt, nt, kt;    // tiles
-    float* partial;        // [splits][batches][M][N or 2 N]
-};
-
 constexpr int TILE = 128;  // C is cut into TILE x TILE (n: 64 outputs for a gated layer's both factors)
 constexpr int LROW = 144;  // bytes of a staged row: 128 of k and a pad that spreads the rows over the banks
 
@@ -90,49 +46,11 @@ __device__ __forceinline__ uintx4 load16(const T* p, int64_t left)
     return v;
 }
 
-template <typename T>
-__device__ __forceinline__ floatx4 product(uintx4 a, uintx4 b, floatx4 c)
-{
-    if constexpr (sizeof(T) == 4) {
-        // four steps of 4: the k index within the 64 bytes is permuted alike on both sides
-        const floatx4 x = __builtin_bit_cast(floatx4, a), y = __builtin_bit_cast(floatx4, b);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(x[i], y[i], c, 0, 0, 0);
-        return c;
-    } else if constexpr (__is_same(T, __bf16)) {
-        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
-    } else {
-        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
-    }
-}
-
 // Row of the staged n side that tile b's instruction row r takes.
 template <bool GATED>
 __device__ __forceinline__ int slot(int b, int r)
 {
     return GATED ? 32 * (b >> 1) + 8 * (r >> 2) + 4 * (b & 1) + (r & 3) : 16 * (r >> 2) + 4 * b + (r & 3);
-}
-
-// Bias, activation, gate, residual of one output, rounded and stored.
-template <typename T, bool GATED>
-__device__ __forceinline__ void finish(const Gemm& g, int64_t batch, int64_t m, int64_t n, float z, float u)
-{
-    const T* bias = static_cast<const T*>(g.bias);
-    if (bias) {
-        z += widen(bias[batch * g.bias_batch + n]);
-        if constexpr (GATED) u += widen(bias[batch * g.bias_batch + g.N + n]);
-    }
-    if (g.pre) {
-        T* pre = static_cast<T*>(g.pre) + batch * g.pre_batch + m * g.pre_row;
-        pre[n] = (T)z;
-        if constexpr (GATED) pre[g.N + n] = (T)u;
-    }
-    float y = act_value(z, g.act);
-    if constexpr (GATED) y *= u;
-    if (g.res) y += widen(static_cast<const T*>(g.res)[batch * g.res_batch + m * g.res_row + n]);
-    const int64_t at = batch * g.c_batch + m * g.c_row + n;
-    if (g.c_dtype == ES_F32) static_cast<float*>(g.c)[at] = y;
-    else static_cast<T*>(g.c)[at] = (T)y;
 }
 
 // 128 bytes of k for `rows` of one operand, staged with k contiguous.
@@ -245,26 +163,23 @@ __global__ __launch_bounds__(256) void k_gemm(GemmArgs a)
         }
     }
 
-    const int64_t wide = GATED ? 2 * (int64_t)g.N : g.N;
+    // a lane's outputs of a row: 16 in a row, or 8 of a gated layer
+    constexpr int W = GATED ? 8 : 16;
+    const int64_t n = GATED ? n0 + 32 * wn + 8 * q : n0 + 64 * wn + 16 * q;
+    float bz[W], bu[W];
+    load_bias<T, GATED, W>(g, batch, n, bz, bu);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int64_t m = m0 + 64 * wm + 16 * i + l16;
         if (m >= g.M) continue;
+        float z[W], u[W];
 #pragma unroll
-        for (int j = 0; j < (GATED ? 2 : 4); ++j)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int64_t n = GATED ? n0 + 32 * wn + 8 * q + 4 * j + e : n0 + 64 * wn + 16 * q + 4 * j + e;
-                if (n >= g.N) continue;
-                const float z = acc[i][j][e], u = GATED ? acc[i][(j + 2) % 4][e] : 0.f;
-                if (a.splits == 1) {
-                    finish<T, GATED>(g, batch, m, n, z, u);
-                } else {
-                    float* p = a.partial + ((split * g.batches + batch) * g.M + m) * wide + n;
-                    p[0] = z;
-                    if constexpr (GATED) p[g.N] = u;
-                }
-            }
+        for (int e = 0; e < W; ++e) {
+            z[e] = acc[i][e / 4][e % 4];
+            u[e] = GATED ? acc[i][(e / 4 + 2) % 4][e % 4] : 0.f;
+        }
+        if (a.splits > 1) store_partial<GATED, W>(a, split, batch, m, n, z, u);
+        else finish<T, GATED, W>(a, batch, m, n, z, u, bz, bu);
     }
 }
 
@@ -276,24 +191,40 @@ __global__ __launch_bounds__(256) void k_gemm_join(GemmArgs a)
     if (id >= g.batches * MN) return;
     const int64_t batch = id / MN, m = id % MN / g.N, n = id % g.N;
     const int64_t wide = GATED ? 2 * (int64_t)g.N : g.N;
-    float z = 0.f, u = 0.f;
+    float z = 0.f, u = 0.f, bz, bu;
     for (int32_t s = 0; s < a.splits; ++s) {
         const float* p = a.partial + ((s * g.batches + batch) * g.M + m) * wide + n;
         z += p[0];
         if constexpr (GATED) u += p[g.N];
     }
-    finish<T, GATED>(g, batch, m, n, z, u);
+    load_bias<T, GATED, 1>(g, batch, n, &bz, &bu);
+    finish<T, GATED, 1>(a, batch, m, n, &z, &u, &bz, &bu);
+}
+
+bool whole(const void* p, int64_t row, int64_t batch, int64_t rows, int64_t batches, size_t elem)
+{
+    return p && reinterpret_cast<uintptr_t>(p) % 16 == 0 && (rows <= 1 || row * elem % 16 == 0) &&
+           (batches <= 1 || batch * elem % 16 == 0);
 }
 
 GemmArgs plan(const Gemm& g)
 {
     GemmArgs a{};
     a.g = g;
-    const int32_t kt = 128 / (int32_t)dtype_size(g.dtype), bn = g.gated ? TILE / 2 : TILE;
+    const size_t e = dtype_size(g.dtype);
+    a.vec_c = whole(g.c, g.c_row, g.c_batch, g.M, g.batches, dtype_size(g.c_dtype));
+    a.vec_res = whole(g.res, g.res_row, g.res_batch, g.M, g.batches, e);
+    a.vec_pre = whole(g.pre, g.pre_row, g.pre_batch, g.M, g.batches, e) && (!g.gated || g.N * e % 16 == 0);
+    a.splits = 1;
+    if (large_fits(g)) {
+        large_plan(a);
+        return a;
+    }
+    const int32_t kt = 128 / (int32_t)e, bn = g.gated ? TILE / 2 : TILE;
+    a.path = PATH_STAGED;
     a.mt = (g.M - 1) / TILE + 1;
     a.nt = (g.N - 1) / bn + 1;
     a.kt = g.K ? (g.K - 1) / kt + 1 : 0;
-    a.splits = 1;
     const int64_t tiles = g.batches * a.mt * a.nt, steps = g.red * a.kt;
     if (tiles < 256 && steps >= 8) {
         const int64_t by_tiles = (512 + tiles - 1) / tiles, by_steps = steps / 4;
@@ -307,11 +238,13 @@ hipError_t launch_typed(const GemmArgs& a, hipStream_t s)
 {
     const Gemm& g = a.g;
     const unsigned grid = (unsigned)(g.batches * a.splits * a.mt * a.nt);
-    if (g.gated) k_gemm<T, true, true, true><<<grid, 256, 0, s>>>(a);
+    hipError_t e = hipSuccess;
+    if (a.path == PATH_LARGE) e = launch_large(a, s);
+    else if (g.gated) k_gemm<T, true, true, true><<<grid, 256, 0, s>>>(a);
     else if (g.a_kmajor && g.b_kmajor) k_gemm<T, true, true, false><<<grid, 256, 0, s>>>(a);
     else if (g.a_kmajor) k_gemm<T, true, false, false><<<grid, 256, 0, s>>>(a);
     else k_gemm<T, false, false, false><<<grid, 256, 0, s>>>(a);
-    hipError_t e = hipGetLastError();
+    if (e == hipSuccess) e = hipGetLastError();
     if (e != hipSuccess || a.splits == 1) return e;
     const unsigned join = (unsigned)((g.batches * g.M * g.N + 255) / 256);
     if (g.gated) k_gemm_join<T, true><<<join, 256, 0, s>>>(a);
@@ -326,6 +259,7 @@ template <typename T, bool GATED>
 __global__ __launch_bounds__(256) void k_gradz(GradZ g, int32_t colblocks, int64_t chunks)
 {
     __shared__ float red[GATED ? 2 : 1][4][64];
+    constexpr bool FAST = sizeof(T) == 2;
     const int64_t wide = GATED ? 2 * (int64_t)g.out : g.out;
     int64_t id = blockIdx.x;
     const int32_t cb = (int32_t)(id % colblocks);
@@ -343,7 +277,7 @@ __global__ __launch_bounds__(256) void k_gradz(GradZ g, int32_t colblocks, int64
             T* dz = static_cast<T*>(g.dz) + (n * g.rows + row) * g.ldz;
             if constexpr (GATED) {
                 const float z = widen(pre[col]), u = widen(pre[g.out + col]);
-                const float dg = d * u * act_slope(z, g.act), du = d * act_value(z, g.act);
+                const float dg = d * u * act_slope<FAST>(z, g.act), du = d * act_value<FAST>(z, g.act);
                 s0 += dg;
                 s1 += du;
                 if (g.dz) {
@@ -351,7 +285,7 @@ __global__ __launch_bounds__(256) void k_gradz(GradZ g, int32_t colblocks, int64
                     dz[g.out + col] = (T)du;
                 }
             } else {
-                const float dd = g.act == ES_ACT_NONE ? d : d * act_slope(widen(pre[col]), g.act);
+                const float dd = g.act == ES_ACT_NONE ? d : d * act_slope<FAST>(widen(pre[col]), g.act);
                 s0 += dd;
                 if (g.dz) dz[col] = (T)dd;
             }

@@ -1,0 +1,225 @@
+// es_dense_device.hpp -- device code that the layer kernels share.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <math.h>
+
+#include "es_dense.hpp"
+
+namespace esmi {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+typedef uint32_t uintx4 __attribute__((ext_vector_type(4)));
+
+// ---- activations ----------------------------------------------------------
+// Evaluated in fp32.  FAST: for results that are rounded to 16 bits (or summed
+// from 16-bit operands), within 4e-7 (1 + |z|) absolute and, towards 0, relative;
+// else the math library's.
+constexpr float LOG2E = 1.44269504088896340736f;
+
+template <bool FAST>
+__device__ __forceinline__ float act_tanh(float z)
+{
+    if constexpr (!FAST) return tanhf(z);
+    // 1 - 2 / (e^2z + 1) loses its leading digits towards 0; the odd Taylor
+    // polynomial to z^7 is within 62/2835 z^8 of tanh z relative: 3e-7 at 1/4
+    const float s = z * z;
+    const float near = z * fmaf(s, fmaf(s, fmaf(s, -17.f / 315.f, 2.f / 15.f), -1.f / 3.f), 1.f);
+    const float far = fmaf(-2.f, __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(z * (2.f * LOG2E)) + 1.f), 1.f);
+    return s < 0.0625f ? near : far;
+}
+
+// Phi(z), the normal distribution function.  FAST: Abramowitz and Stegun
+// 7.1.26, erfc x = t (a1 + ... + a5 t^4) e^(-x^2), t = 1 / (1 + p x), x >= 0,
+// within 1.5e-7.
+template <bool FAST>
+__device__ __forceinline__ float normal_cdf(float z, float e /* e^(-z^2/2), FAST only */)
+{
+    if constexpr (!FAST) return 0.5f * erfcf(-0.70710678118654752440f * z);
+    const float x = __builtin_fabsf(z) * 0.70710678118654752440f;
+    const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, x, 1.f));
+    const float p = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
+    const float half = 0.5f * p * e;
+    return z < 0.f ? half : 1.f - half;
+}
+
+template <bool FAST>
+__device__ __forceinline__ float bell(float z)  // e^(-z^2/2)
+{
+    if constexpr (!FAST) return expf(-0.5f * z * z);
+    return __builtin_amdgcn_exp2f(z * z * (-0.5f * LOG2E));
+}
+
+template <bool FAST>
+__device__ __forceinline__ float sigmoid(float z)
+{
+    if constexpr (!FAST) return 1.f / (1.f + expf(-z));
+    return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * -LOG2E));
+}
+
+template <bool FAST>
+__device__ __forceinline__ float act_value(float z, int32_t act)
+{
+    switch (act) {
+    case ES_ACT_RELU: return z <= 0.f ? 0.f : z;  // NaN stays
+    case ES_ACT_TANH: return act_tanh<FAST>(z);
+    case ES_ACT_GELU: return z * normal_cdf<FAST>(z, FAST ? bell<FAST>(z) : 0.f);
+    case ES_ACT_SILU: return z * sigmoid<FAST>(z);
+    default: return z;
+    }
+}
+
+template <bool FAST>
+__device__ __forceinline__ float act_slope(float z, int32_t act)
+{
+    switch (act) {
+    case ES_ACT_RELU: return z > 0.f ? 1.f : z != z ? z : 0.f;
+    case ES_ACT_TANH: {
+        const float t = act_tanh<FAST>(z);
+        return (1.f - t) * (1.f + t);
+    }
+    case ES_ACT_GELU: {
+        const float e = bell<FAST>(z);
+        return fmaf(z * e, 0.39894228040143267794f, normal_cdf<FAST>(z, e));
+    }
+    case ES_ACT_SILU: {
+        const float s = sigmoid<FAST>(z);
+        return s * fmaf(z, 1.f - s, 1.f);
+    }
+    default: return 1.f;
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ float widen(T v) { return (float)v; }
+
+template <typename T>
+__device__ __forceinline__ floatx4 product(uintx4 a, uintx4 b, floatx4 c)
+{
+    if constexpr (sizeof(T) == 4) {
+        // four steps of 4: the k index within the 64 bytes is permuted alike on both sides
+        const floatx4 x = __builtin_bit_cast(floatx4, a), y = __builtin_bit_cast(floatx4, b);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(x[i], y[i], c, 0, 0, 0);
+        return c;
+    } else if constexpr (__is_same(T, __bf16)) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    } else {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+    }
+}
+
+// ---- a product's launch ---------------------------------------------------
+enum GemmPath { PATH_STAGED, PATH_LARGE };
+
+struct GemmArgs {
+    Gemm g;
+    int32_t path;
+    int32_t splits;        // of the reduction; 1: C is finished here
+    int32_t mt, nt, kt;    // tiles
+    int32_t per;           // steps of a split (large tiles)
+    bool vec_c, vec_res, vec_pre;  // rows take 16-byte pieces
+    float* partial;        // [splits][batches][M][N or 2 N]
+};
+
+// W consecutive elements of a row, `left` of them in it
+template <typename T, int W>
+__device__ __forceinline__ void load_run(const T* p, bool vec, int64_t left, float out[W])
+{
+    if (vec && left >= W) {
+        T t[W];
+        __builtin_memcpy(t, __builtin_assume_aligned(p, W * sizeof(T) < 16 ? W * sizeof(T) : 16), W * sizeof(T));
+#pragma unroll
+        for (int i = 0; i < W; ++i) out[i] = widen(t[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < W; ++i) out[i] = i < left ? widen(p[i]) : 0.f;
+    }
+}
+
+template <typename T, int W>
+__device__ __forceinline__ void store_run(T* p, bool vec, int64_t left, const float v[W])
+{
+    if (vec && left >= W) {
+        T t[W];
+#pragma unroll
+        for (int i = 0; i < W; ++i) t[i] = (T)v[i];
+        __builtin_memcpy(__builtin_assume_aligned(p, W * sizeof(T) < 16 ? W * sizeof(T) : 16), t, W * sizeof(T));
+    } else {
+#pragma unroll
+        for (int i = 0; i < W; ++i)
+            if (i < left) p[i] = (T)v[i];
+    }
+}
+
+// Bias, activation, gate and residual of W consecutive outputs from column n
+// of row m, rounded and stored.  bz, bu: their biases.
+template <typename T, bool GATED, int W>
+__device__ __forceinline__ void finish(const GemmArgs& a, int64_t batch, int64_t m, int64_t n, float z[W], float u[W],
+                                       const float bz[W], const float bu[W])
+{
+    const Gemm& g = a.g;
+    constexpr bool FAST = sizeof(T) == 2;
+    const int64_t left = g.N - n;
+    if (left <= 0) return;
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+        z[i] += bz[i];
+        if constexpr (GATED) u[i] += bu[i];
+    }
+    if (g.pre) {
+        T* pre = static_cast<T*>(g.pre) + batch * g.pre_batch + m * g.pre_row + n;
+        store_run<T, W>(pre, a.vec_pre, left, z);
+        if constexpr (GATED) store_run<T, W>(pre + g.N, a.vec_pre, left, u);
+    }
+    if (g.act != ES_ACT_NONE) {
+#pragma unroll
+        for (int i = 0; i < W; ++i) z[i] = act_value<FAST>(z[i], g.act);
+    }
+    if constexpr (GATED) {
+#pragma unroll
+        for (int i = 0; i < W; ++i) z[i] *= u[i];
+    }
+    if (g.res) {
+        float r[W];
+        load_run<T, W>(static_cast<const T*>(g.res) + batch * g.res_batch + m * g.res_row + n, a.vec_res, left, r);
+#pragma unroll
+        for (int i = 0; i < W; ++i) z[i] += r[i];
+    }
+    const int64_t at = batch * g.c_batch + m * g.c_row + n;
+    if (g.c_dtype == ES_F32) store_run<float, W>(static_cast<float*>(g.c) + at, a.vec_c, left, z);
+    else store_run<T, W>(static_cast<T*>(g.c) + at, a.vec_c, left, z);
+}
+
+template <typename T, bool GATED, int W>
+__device__ __forceinline__ void load_bias(const Gemm& g, int64_t batch, int64_t n, float bz[W], float bu[W])
+{
+#pragma unroll
+    for (int i = 0; i < W; ++i) bz[i] = bu[i] = 0.f;
+    if (!g.bias || n >= g.N) return;
+    const T* b = static_cast<const T*>(g.bias) + batch * g.bias_batch + n;
+    load_run<T, W>(b, false, g.N - n, bz);
+    if constexpr (GATED) load_run<T, W>(b + g.N, false, g.N - n, bu);
+}
+
+// Partial sums of W consecutive outputs
+template <bool GATED, int W>
+__device__ __forceinline__ void store_partial(const GemmArgs& a, int32_t split, int64_t batch, int64_t m, int64_t n,
+                                              const float z[W], const float u[W])
+{
+    const Gemm& g = a.g;
+    const int64_t left = g.N - n;
+    if (left <= 0) return;
+    float* p = a.partial + ((split * g.batches + batch) * g.M + m) * (GATED ? 2 * (int64_t)g.N : g.N) + n;
+    const bool vec = g.N % 4 == 0;
+    store_run<float, W>(p, vec, left, z);
+    if constexpr (GATED) store_run<float, W>(p + g.N, vec, left, u);
+}
+
+bool large_fits(const Gemm& g);
+void large_plan(GemmArgs& a);
+hipError_t launch_large(const GemmArgs& a, hipStream_t s);
+
+}  // namespace esmi
