@@ -14,7 +14,7 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libesmi.so")
-SOURCES = ["es_kernels.hip", "es_mlp.hip", "es_rank_sort.hip", "es_dense.hip", "es_dense_large.hip", "es_adamw.hip", "es_layers.cpp",
+SOURCES = ["es_kernels.hip", "es_mlp.hip", "es_rank_sort.hip", "es_dense.hip", "es_dense_large.hip", "es_dense_rows.hip", "es_adamw.hip", "es_layers.cpp",
            "es_api.cpp"]
 ARCH = "gfx950"
 

@@ -179,7 +179,11 @@ __global__ __launch_bounds__(256) void k_gemm(GemmArgs a)
             u[e] = GATED ? acc[i][(e / 4 + 2) % 4][e % 4] : 0.f;
         }
         if (a.splits > 1) store_partial<GATED, W>(a, split, batch, m, n, z, u);
-        else finish<T, GATED, W>(a, batch, m, n, z, u, bz, bu);
+        else {
+            float r[W];
+            load_res<T, W>(a, batch, m, n, r);
+            finish<T, GATED, W>(a, batch, m, n, z, u, bz, bu, r);
+        }
     }
 }
 
@@ -191,14 +195,15 @@ __global__ __launch_bounds__(256) void k_gemm_join(GemmArgs a)
     if (id >= g.batches * MN) return;
     const int64_t batch = id / MN, m = id % MN / g.N, n = id % g.N;
     const int64_t wide = GATED ? 2 * (int64_t)g.N : g.N;
-    float z = 0.f, u = 0.f, bz, bu;
+    float z = 0.f, u = 0.f, bz, bu, r;
+    load_bias<T, GATED, 1>(g, batch, n, &bz, &bu);
+    load_res<T, 1>(a, batch, m, n, &r);
     for (int32_t s = 0; s < a.splits; ++s) {
         const float* p = a.partial + ((s * g.batches + batch) * g.M + m) * wide + n;
         z += p[0];
         if constexpr (GATED) u += p[g.N];
     }
-    load_bias<T, GATED, 1>(g, batch, n, &bz, &bu);
-    finish<T, GATED, 1>(a, batch, m, n, &z, &u, &bz, &bu);
+    finish<T, GATED, 1>(a, batch, m, n, &z, &u, &bz, &bu, &r);
 }
 
 bool whole(const void* p, int64_t row, int64_t batch, int64_t rows, int64_t batches, size_t elem)
@@ -216,6 +221,10 @@ GemmArgs plan(const Gemm& g)
     a.vec_res = whole(g.res, g.res_row, g.res_batch, g.M, g.batches, e);
     a.vec_pre = whole(g.pre, g.pre_row, g.pre_batch, g.M, g.batches, e) && (!g.gated || g.N * e % 16 == 0);
     a.splits = 1;
+    if (rows_fits(g)) {
+        rows_plan(a);
+        return a;
+    }
     if (large_fits(g)) {
         large_plan(a);
         return a;
@@ -237,6 +246,7 @@ template <typename T>
 hipError_t launch_typed(const GemmArgs& a, hipStream_t s)
 {
     const Gemm& g = a.g;
+    if (a.path == PATH_ROWS) return launch_rows(a, s);
     const unsigned grid = (unsigned)(g.batches * a.splits * a.mt * a.nt);
     hipError_t e = hipSuccess;
     if (a.path == PATH_LARGE) e = launch_large(a, s);
@@ -321,13 +331,14 @@ __global__ __launch_bounds__(256) void k_bias_grad(const float* sums, int64_t me
 size_t gemm_workspace_floats(const Gemm& g)
 {
     const GemmArgs a = plan(g);
-    return a.splits > 1 ? (size_t)a.splits * g.batches * g.M * (g.gated ? 2 : 1) * (size_t)g.N : 0;
+    return a.path != PATH_ROWS && a.splits > 1 ? (size_t)a.splits * g.batches * g.M * (g.gated ? 2 : 1) * (size_t)g.N : 0;
 }
 
 bool gemm_too_large(const Gemm& g)
 {
     const GemmArgs a = plan(g);
     const __int128 most = 0x7FFFFFFF;
+    if (a.path == PATH_ROWS) return (__int128)g.batches * a.nt > most;
     return (__int128)g.batches * a.splits * a.mt * a.nt > most ||
            (a.splits > 1 && (__int128)g.batches * g.M * g.N / 256 >= most);
 }

@@ -112,19 +112,19 @@ __device__ __forceinline__ floatx4 product(uintx4 a, uintx4 b, floatx4 c)
 }
 
 // ---- a product's launch ---------------------------------------------------
-enum GemmPath { PATH_STAGED, PATH_LARGE };
+enum GemmPath { PATH_STAGED, PATH_LARGE, PATH_ROWS };
 
 struct GemmArgs {
     Gemm g;
     int32_t path;
-    int32_t splits;        // of the reduction; 1: C is finished here
+    int32_t splits;        // of the reduction; 1: C is finished here (few rows: among a workgroup's waves)
     int32_t mt, nt, kt;    // tiles
-    int32_t per;           // steps of a split (large tiles)
+    int32_t per;           // steps of a split
     bool vec_c, vec_res, vec_pre;  // rows take 16-byte pieces
     float* partial;        // [splits][batches][M][N or 2 N]
 };
 
-// W consecutive elements of a row, `left` of them in it
+// W consecutive elements of a row, `left` > 0 of them in it (the others repeat its last)
 template <typename T, int W>
 __device__ __forceinline__ void load_run(const T* p, bool vec, int64_t left, float out[W])
 {
@@ -135,7 +135,7 @@ __device__ __forceinline__ void load_run(const T* p, bool vec, int64_t left, flo
         for (int i = 0; i < W; ++i) out[i] = widen(t[i]);
     } else {
 #pragma unroll
-        for (int i = 0; i < W; ++i) out[i] = i < left ? widen(p[i]) : 0.f;
+        for (int i = 0; i < W; ++i) out[i] = widen(p[i < left ? i : left - 1]);  // no branches: all in flight at once
     }
 }
 
@@ -154,11 +154,23 @@ __device__ __forceinline__ void store_run(T* p, bool vec, int64_t left, const fl
     }
 }
 
+// The residual of W consecutive outputs from column n of row m
+template <typename T, int W>
+__device__ __forceinline__ void load_res(const GemmArgs& a, int64_t batch, int64_t m, int64_t n, float r[W])
+{
+    const Gemm& g = a.g;
+    if (g.res && n < g.N)
+        load_run<T, W>(static_cast<const T*>(g.res) + batch * g.res_batch + m * g.res_row + n, a.vec_res, g.N - n, r);
+    else
+#pragma unroll
+        for (int i = 0; i < W; ++i) r[i] = 0.f;
+}
+
 // Bias, activation, gate and residual of W consecutive outputs from column n
-// of row m, rounded and stored.  bz, bu: their biases.
+// of row m, rounded and stored.  bz, bu: their biases, r: the residual.
 template <typename T, bool GATED, int W>
 __device__ __forceinline__ void finish(const GemmArgs& a, int64_t batch, int64_t m, int64_t n, float z[W], float u[W],
-                                       const float bz[W], const float bu[W])
+                                       const float bz[W], const float bu[W], const float r[W])
 {
     const Gemm& g = a.g;
     constexpr bool FAST = sizeof(T) == 2;
@@ -183,8 +195,6 @@ __device__ __forceinline__ void finish(const GemmArgs& a, int64_t batch, int64_t
         for (int i = 0; i < W; ++i) z[i] *= u[i];
     }
     if (g.res) {
-        float r[W];
-        load_run<T, W>(static_cast<const T*>(g.res) + batch * g.res_batch + m * g.res_row + n, a.vec_res, left, r);
 #pragma unroll
         for (int i = 0; i < W; ++i) z[i] += r[i];
     }
@@ -218,6 +228,9 @@ __device__ __forceinline__ void store_partial(const GemmArgs& a, int32_t split, 
     if constexpr (GATED) store_run<float, W>(p + g.N, vec, left, u);
 }
 
+bool rows_fits(const Gemm& g);
+void rows_plan(GemmArgs& a);
+hipError_t launch_rows(const GemmArgs& a, hipStream_t s);
 bool large_fits(const Gemm& g);
 void large_plan(GemmArgs& a);
 hipError_t launch_large(const GemmArgs& a, hipStream_t s);

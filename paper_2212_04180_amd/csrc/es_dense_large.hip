@@ -230,7 +230,11 @@ __global__ __launch_bounds__(256, 2) void k_gemm_large(GemmArgs a)
                 u[e] = GATED ? acc[i][(e / 4 + 2) % 4][e % 4] : 0.f;
             }
             if (a.splits > 1) store_partial<GATED, W>(a, split, batch, m, n, z, u);
-            else finish<T, GATED, W>(a, batch, m, n, z, u, bz, bu);
+            else {
+                float r[W];
+                load_res<T, W>(a, batch, m, n, r);
+                finish<T, GATED, W>(a, batch, m, n, z, u, bz, bu, r);
+            }
         }
     }
 }

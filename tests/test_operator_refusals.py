@@ -99,8 +99,8 @@ def test_backward(name, gated):
         assert _query(name, _backward(act=0, pre_p=0))[0] == esmi.ES_OK
 
 
-@pytest.mark.parametrize("packed,name", [(_backward(), "es_dense_backward"), (_backward(True), "es_gated_backward"),
-                                         (_forward(members=1, rows=4, y_row=64, residual_row=64, pre_row=64, out=64, x_row=60000,
+@pytest.mark.parametrize("packed,name", ids=["dense_backward", "gated_backward", "dense"], argvalues=[(_backward(), "es_dense_backward"), (_backward(True), "es_gated_backward"),
+                                         (_forward(members=1, rows=40, y_row=64, residual_row=64, pre_row=64, out=64, x_row=60000,
                                                    w_row=60000, **{"in": 60000}), "es_dense")])
 def test_workspace_must_fit(packed, name):
     rc, n, _ = _query(name, packed)
