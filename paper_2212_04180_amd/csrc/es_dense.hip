@@ -10,13 +10,11 @@
 // The matrix cores hold D = A B with the rows of B^T as the lanes: the n side
 // (outputs) is the instruction's A operand and the m side (inputs' rows) its B
 // operand, so that a lane's four accumulators of a tile lie in one row of C.
-// A wave owns 64 x 64 of C as 4 x 4 tiles; tile b of the n side takes the rows
-// n = 16 (r / 4) + 4 b + r % 4 of its 64 (r: row of the instruction), so that a
-// lane ends with 16 consecutive outputs of a row, stored in 16-byte pieces.
-// A gated layer's 64 are 32 gates and the 32 matching others, and a lane has
-// both factors of 8 consecutive outputs.
+// A gated layer's columns of a wave are half gates and half the matching others.
 #include <hip/hip_runtime.h>
 #include <math.h>
+
+#include <algorithm>
 
 #include "es_dense.hpp"
 #include "es_dense_device.hpp"
@@ -26,184 +24,239 @@ namespace esmi {
 namespace {
 
 // ---- the product ----------------------------------------------------------
-constexpr int TILE = 128;  // C is cut into TILE x TILE (n: 64 outputs for a gated layer's both factors)
-constexpr int LROW = 144;  // bytes of a staged row: 128 of k and a pad that spreads the rows over the banks
+// Any type, size, stride and alignment.  Four waves make a TS x TS tile of C (TS
+// 128, or 64 where there are few tiles), (TS / 2)^2 each.  A step is 128 bytes
+// of k: fetched into registers while the step before is multiplied, then
+// staged in LDS.  An operand with k contiguous is staged row by row and read 16
+// bytes a lane; piece c of row r lies at c ^ f(r), which spreads the lanes that a
+// 16-byte read serves together ({0-3, 12-15, 20-27}, {4-11, 16-19, 28-31} and
+// those + 32, measured) over all banks.
+// Another one is staged as it lies, a row of m (n) per k: 16-bit fragments come
+// back transposed by ds_read_b64_tr_b16 (lane i of 16 gets the four k of column
+// i), fp32 ones word by word.
+template <typename T, bool KMAJOR, int TS>
+struct Staged {
+    static constexpr int E = 16 / sizeof(T), KT = 128 / sizeof(T), LOADS = TS * 8 / 256;
+    // fp32: rows 4 apart lie 16 banks apart
+    static constexpr int ROW = KMAJOR ? 128 : TS * (int)sizeof(T) + (sizeof(T) == 4 ? 16 : 32);
+    static constexpr int BYTES = (KMAJOR ? TS : KT) * ROW;
+    const T* p[LOADS];
+    int32_t left[LOADS];  // not k-major: valid columns from p
+    uintx4 v[LOADS];
 
-// 16 bytes of a row from any address, zeros behind `left` elements
-template <typename T>
-__device__ __forceinline__ uintx4 load16(const T* p, int64_t left)
-{
-    constexpr int E = 16 / sizeof(T);
-    uintx4 v = {0, 0, 0, 0};
-    if (left >= E) {
-        __builtin_memcpy(&v, p, 16);
-    } else {
-        T t[E];
-#pragma unroll
-        for (int i = 0; i < E; ++i) t[i] = i < left ? p[i] : (T)0.f;
-        __builtin_memcpy(&v, t, 16);
+    static __device__ __forceinline__ int f(int row)
+    {
+        const int a = (row >> 2) & 3;
+        return (2 * a + ((row >> 1) & 1)) ^ ((a ^ (a >> 1)) & 1);
     }
-    return v;
-}
 
-// Row of the staged n side that tile b's instruction row r takes.
-template <bool GATED>
-__device__ __forceinline__ int slot(int b, int r)
-{
-    return GATED ? 32 * (b >> 1) + 8 * (r >> 2) + 4 * (b & 1) + (r & 3) : 16 * (r >> 2) + 4 * b + (r & 3);
-}
-
-// 128 bytes of k for `rows` of one operand, staged with k contiguous.
-template <typename T, bool KMAJOR, bool GATED>
-struct Stage {
-    static constexpr int E = 16 / sizeof(T), BK = 128 / sizeof(T);
-    uintx4 v[4];
-
-    // row `i` of the staged 128 is memory row (or column) row_of(i), -1: none
+    // row_of(i): the matrix's row of staged row i (inside), or, not k-major, its first column and how many are left
     template <typename F>
-    __device__ __forceinline__ void load(const T* base, int64_t stride, int32_t k0, int32_t K, int32_t limit, F row_of)
+    __device__ __forceinline__ void init(const T* base, int64_t stride, F row_of)
     {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < LOADS; ++j) {
             const int c = (int)threadIdx.x + 256 * j;
-            v[j] = uintx4{0, 0, 0, 0};
+            int32_t n;
             if constexpr (KMAJOR) {
-                const int64_t row = row_of(c / 8);
-                const int32_t k = k0 + (c % 8) * E;
-                if (row >= 0 && k < K) v[j] = load16(base + row * stride + k, K - k);
+                p[j] = base + row_of(c / 8, n) * stride + (c % 8) * E;
             } else {
-                constexpr int PER = TILE / E;  // pieces of a k row
-                const int32_t k = k0 + c / PER;
-                const int64_t row = row_of((c % PER) * E);
-                if (row >= 0 && k < K) v[j] = load16(base + (int64_t)k * stride + row, limit - row);
+                constexpr int PER = TS / E;
+                const int64_t col = row_of((c % PER) * E, n);
+                left[j] = n;
+                p[j] = base + (int64_t)(c / PER) * stride + col;
+            }
+        }
+    }
+    // the step whose first k has `k_left` behind it, `at` elements from the first
+    __device__ __forceinline__ void fetch(int64_t at, int32_t k_left)
+    {
+#pragma unroll
+        for (int j = 0; j < LOADS; ++j) {
+            const int c = (int)threadIdx.x + 256 * j;
+            int n;  // elements to read
+            if constexpr (KMAJOR) n = k_left - (c % 8) * E;
+            else n = c / (TS / E) < k_left ? left[j] : 0;
+            if (n >= E) {
+                __builtin_memcpy(&v[j], p[j] + at, 16);
+            } else {
+                T t[E];
+#pragma unroll
+                for (int i = 0; i < E; ++i) t[i] = i < n ? p[j][at + i] : (T)0.f;
+                __builtin_memcpy(&v[j], t, 16);
             }
         }
     }
     __device__ __forceinline__ void store(unsigned char* lds) const
     {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < LOADS; ++j) {
             const int c = (int)threadIdx.x + 256 * j;
-            if constexpr (KMAJOR) {
-                *reinterpret_cast<uintx4*>(lds + (c / 8) * LROW + (c % 8) * 16) = v[j];
-            } else {
-                constexpr int PER = TILE / E;
-                T t[E];
-                __builtin_memcpy(t, &v[j], 16);
+            const int at = KMAJOR ? (c / 8) * ROW + ((c % 8) ^ f(c / 8)) * 16 : (c / (TS / E)) * ROW + (c % (TS / E)) * 16;
+            *reinterpret_cast<uintx4*>(lds + at) = v[j];
+        }
+    }
+    // fragment `ks` (64 bytes of k) of staged rows (columns) base + l16
+    static __device__ __forceinline__ uintx4 read(const unsigned char* lds, int base, int ks, int lane)
+    {
+        const int l16 = lane % 16, q = lane / 16;
+        if constexpr (KMAJOR) {
+            return *reinterpret_cast<const uintx4*>(lds + (base + l16) * ROW + ((4 * ks + q) ^ f(base + l16)) * 16);
+        } else if constexpr (sizeof(T) == 4) {
+            uintx4 v;
 #pragma unroll
-                for (int i = 0; i < E; ++i)
-                    *reinterpret_cast<T*>(lds + ((c % PER) * E + i) * LROW + (c / PER) * (int)sizeof(T)) = t[i];
+            for (int i = 0; i < 4; ++i)
+                v[i] = *reinterpret_cast<const uint32_t*>(lds + (16 * ks + 4 * q + i) * ROW + (base + l16) * 4);
+            return v;
+        } else {
+            typedef short shortx4 __attribute__((ext_vector_type(4)));
+            shortx4 t[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const unsigned char* at = lds + (32 * ks + 8 * q + 4 * h + (l16 >> 2)) * ROW + (base + 4 * (l16 & 3)) * 2;
+                t[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) shortx4*)at);
             }
+            uintx4 v;
+            __builtin_memcpy(&v, t, 16);
+            return v;
         }
     }
 };
 
-template <typename T, bool AK, bool BK, bool GATED>
+template <typename T, bool AK, bool BK, bool GATED, int TS>
 __global__ __launch_bounds__(256) void k_gemm(GemmArgs a)
 {
-    __shared__ __align__(16) unsigned char sa[TILE * LROW], sb[TILE * LROW];
+    using SA = Staged<T, AK, TS>;
+    using SB = Staged<T, BK, TS>;
+    constexpr int KT = 128 / sizeof(T), HALF = TS / 2, NT = TS / 32;  // NT: 16 x 16 tiles of a wave, each way
+    constexpr int OUTS = GATED ? HALF : TS, STAGED = SA::BYTES + SB::BYTES, FINAL = 4 * EPILOGUE_LDS<NT>;
+    __shared__ __align__(16) unsigned char lds[STAGED > FINAL ? STAGED : FINAL];
+    unsigned char *sa = lds, *sb = lds + SA::BYTES;
     const Gemm& g = a.g;
-    constexpr int KT = 128 / sizeof(T);
-    constexpr int BN = GATED ? TILE / 2 : TILE;
-    int64_t id = blockIdx.x;
-    const int32_t tn = (int32_t)(id % a.nt);
+    uint32_t id = blockIdx.x;
+    const int32_t tn = id % a.nt;
     id /= a.nt;
-    const int32_t tm = (int32_t)(id % a.mt);
+    const int32_t tm = id % a.mt;
     id /= a.mt;
-    const int32_t split = (int32_t)(id % a.splits);
-    const int64_t batch = id / a.splits;
-    const int32_t m0 = tm * TILE, n0 = tn * BN;
-    const int wave = threadIdx.x / 64, lane = threadIdx.x % 64, q = lane / 16, l16 = lane % 16;
+    const int64_t split = id % (uint32_t)a.splits, batch = id / (uint32_t)a.splits;
+    const int32_t m0 = tm * TS, n0 = tn * OUTS;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
     const int wm = wave / 2, wn = wave % 2;
-    const int64_t steps = g.red * a.kt, first = steps * split / a.splits, last = steps * (split + 1) / a.splits;
-    const T* A = static_cast<const T*>(g.a) + batch * g.a_batch;
-    const T* B = static_cast<const T*>(g.b) + batch * g.b_batch;
-    auto row_a = [&](int i) -> int64_t { return m0 + i < g.M ? m0 + i : -1; };
-    auto row_b = [&](int i) -> int64_t {
+    const int64_t steps = g.red * a.kt, first = split * a.per, last = steps - first < a.per ? steps : first + a.per;
+    int64_t r = a.splits > 1 ? first / a.kt : 0;
+    int32_t kt = (int32_t)(first - r * a.kt);
+    SA va;
+    SB vb;
+    // rows behind the last are read as the last: what they give is not stored
+    va.init(static_cast<const T*>(g.a) + batch * g.a_batch + r * g.a_red, g.a_row, [&](int i, int32_t& n) -> int64_t {
+        n = g.M - m0 - i;
+        return AK && n <= 0 ? g.M - 1 : m0 + i;
+    });
+    vb.init(static_cast<const T*>(g.b) + batch * g.b_batch + r * g.b_red, g.b_row, [&](int i, int32_t& n) -> int64_t {
         if constexpr (GATED) {
-            const int32_t n = n0 + 32 * (i / 64) + i % 32;
-            return n < g.N ? n + (i / 32 % 2 ? (int64_t)g.N : 0) : -1;
+            // a wave's rows: the gates, then the others
+            const int32_t o = n0 + HALF / 2 * (i / HALF) + i % (HALF / 2);
+            return (o < g.N ? o : g.N - 1) + (i / (HALF / 2) % 2 ? (int64_t)g.N : 0);
         } else {
-            return n0 + i < g.N ? n0 + i : -1;
+            n = g.N - n0 - i;
+            return BK && n <= 0 ? g.N - 1 : n0 + i;
+        }
+    });
+
+    floatx4 acc[NT][NT];  // [m tile][n tile]
+#pragma unroll
+    for (int i = 0; i < NT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+    int64_t ra = 0, rb = 0;  // the reduction batch's offsets from r's
+    auto fetch = [&]() {
+        const int32_t k0 = kt * KT;
+        va.fetch(ra + (AK ? (int64_t)k0 : k0 * g.a_row), g.K - k0);
+        vb.fetch(rb + (BK ? (int64_t)k0 : k0 * g.b_row), g.K - k0);
+        if (++kt == a.kt) {
+            kt = 0;
+            ra += g.a_red;
+            rb += g.b_red;
         }
     };
-
-    floatx4 acc[4][4];  // [m tile][n tile]
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
-    Stage<T, AK, false> va;
-    Stage<T, BK, GATED> vb;
-    auto fetch = [&](int64_t t) {
-        const int64_t r = t / a.kt;
-        const int32_t k0 = (int32_t)(t % a.kt) * KT;
-        va.load(A + r * g.a_red, g.a_row, k0, g.K, g.M, row_a);
-        vb.load(B + r * g.b_red, g.b_row, k0, g.K, g.N, row_b);
-    };
-    if (first < last) fetch(first);
+    if (first < last) fetch();
     for (int64_t t = first; t < last; ++t) {
         __syncthreads();
         va.store(sa);
         vb.store(sb);
         __syncthreads();
-        if (t + 1 < last) fetch(t + 1);
+        if (t + 1 < last) fetch();
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
-            uintx4 fa[4], fb[4];
+            uintx4 fa[NT], fb[NT];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                fa[i] = *reinterpret_cast<const uintx4*>(sa + (64 * wm + 16 * i + l16) * LROW + ks * 64 + q * 16);
-                fb[i] = *reinterpret_cast<const uintx4*>(sb + (64 * wn + slot<GATED>(i, l16)) * LROW + ks * 64 + q * 16);
+            for (int i = 0; i < NT; ++i) {
+                fa[i] = SA::read(sa, HALF * wm + 16 * i, ks, lane);
+                fb[i] = SB::read(sb, HALF * wn + 16 * i, ks, lane);
             }
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int i = 0; i < NT; ++i)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) acc[i][j] = product<T>(fb[j], fa[i], acc[i][j]);
+                for (int j = 0; j < NT; ++j) acc[i][j] = product<T>(fb[j], fa[i], acc[i][j]);
         }
     }
 
-    // a lane's outputs of a row: 16 in a row, or 8 of a gated layer
-    constexpr int W = GATED ? 8 : 16;
-    const int64_t n = GATED ? n0 + 32 * wn + 8 * q : n0 + 64 * wn + 16 * q;
-    float bz[W], bu[W];
-    load_bias<T, GATED, W>(g, batch, n, bz, bu);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int64_t m = m0 + 64 * wm + 16 * i + l16;
-        if (m >= g.M) continue;
-        float z[W], u[W];
-#pragma unroll
-        for (int e = 0; e < W; ++e) {
-            z[e] = acc[i][e / 4][e % 4];
-            u[e] = GATED ? acc[i][(e / 4 + 2) % 4][e % 4] : 0.f;
-        }
-        if (a.splits > 1) store_partial<GATED, W>(a, split, batch, m, n, z, u);
-        else {
-            float r[W];
-            load_res<T, W>(a, batch, m, n, r);
-            finish<T, GATED, W>(a, batch, m, n, z, u, bz, bu, r);
-        }
-    }
+    __syncthreads();  // the staged steps make room for the epilogue
+    epilogue<T, GATED, NT, NT>(a, (int32_t)split, batch, m0 + HALF * wm, n0 + (GATED ? HALF / 2 : HALF) * wn, acc,
+                               reinterpret_cast<float*>(lds + wave * EPILOGUE_LDS<NT>), lane);
 }
 
+// Sums of the splits and the epilogue, four outputs a thread.  Few outputs leave
+// the chip idle: `slices` threads then share one's splits, each in its order.
 template <typename T, bool GATED>
-__global__ __launch_bounds__(256) void k_gemm_join(GemmArgs a)
+__global__ __launch_bounds__(256) void k_gemm_join(GemmArgs a, int64_t total, uint32_t quads, int32_t slices)
 {
+    __shared__ floatx4 red[GATED ? 2 : 1][256];
     const Gemm& g = a.g;
-    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x, MN = (int64_t)g.M * g.N;
-    if (id >= g.batches * MN) return;
-    const int64_t batch = id / MN, m = id % MN / g.N, n = id % g.N;
-    const int64_t wide = GATED ? 2 * (int64_t)g.N : g.N;
-    float z = 0.f, u = 0.f, bz, bu, r;
-    load_bias<T, GATED, 1>(g, batch, n, &bz, &bu);
-    load_res<T, 1>(a, batch, m, n, &r);
-    for (int32_t s = 0; s < a.splits; ++s) {
-        const float* p = a.partial + ((s * g.batches + batch) * g.M + m) * wide + n;
-        z += p[0];
-        if constexpr (GATED) u += p[g.N];
+    const int per = 256 / slices, slice = (int)threadIdx.x / per;
+    const int64_t id = (int64_t)blockIdx.x * per + threadIdx.x % per;  // [batch][m][quad of outputs]
+    const bool inside = id < total;
+    const int64_t row = !inside ? 0 : total <= 0xFFFFFFFFll ? (uint32_t)id / quads : id / quads;
+    const int64_t batch = total <= 0xFFFFFFFFll ? (uint32_t)row / (uint32_t)g.M : row / g.M;
+    const int32_t o = inside ? (int32_t)((id - row * quads) * 4) : 0, left = g.N - o;
+    const int64_t m = row - batch * g.M, wide = GATED ? 2 * (int64_t)g.N : g.N;
+    const bool vec = g.N % 4 == 0;
+    float z[4] = {}, u[4] = {}, bz[4], bu[4], r[4];
+    if (slice == 0) {
+        load_bias<T, GATED, 4>(g, batch, o, bz, bu);
+        load_res<T, 4>(a, batch, m, o, r);
     }
-    finish<T, GATED, 1>(a, batch, m, n, &z, &u, &bz, &bu, &r);
+    const int64_t pitch = g.batches * g.M * wide;
+    const float* p = a.partial + row * wide + o + slice * pitch;
+#pragma unroll 4
+    for (int32_t s = slice; s < a.splits; s += slices, p += slices * pitch) {
+        float v[4];
+        load_run<float, 4>(p, vec, left, v);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) z[i] += v[i];
+        if constexpr (GATED) {
+            load_run<float, 4>(p + g.N, vec, left, v);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) u[i] += v[i];
+        }
+    }
+    if (slices > 1) {
+        red[0][threadIdx.x] = floatx4{z[0], z[1], z[2], z[3]};
+        if constexpr (GATED) red[GATED][threadIdx.x] = floatx4{u[0], u[1], u[2], u[3]};
+        __syncthreads();
+        if (slice) return;
+        for (int s = 1; s < slices; ++s) {
+            const floatx4 v = red[0][threadIdx.x + s * per];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) z[i] += v[i];
+            if constexpr (GATED) {
+                const floatx4 w = red[GATED][threadIdx.x + s * per];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) u[i] += w[i];
+            }
+        }
+    }
+    if (inside) finish<T, GATED, 4>(a, batch, m, o, z, u, bz, bu, r);
 }
 
 bool whole(const void* p, int64_t row, int64_t batch, int64_t rows, int64_t batches, size_t elem)
@@ -229,18 +282,36 @@ GemmArgs plan(const Gemm& g)
         large_plan(a);
         return a;
     }
-    const int32_t kt = 128 / (int32_t)e, bn = g.gated ? TILE / 2 : TILE;
+    const int32_t kt = 128 / (int32_t)e;
     a.path = PATH_STAGED;
-    a.mt = (g.M - 1) / TILE + 1;
-    a.nt = (g.N - 1) / bn + 1;
     a.kt = g.K ? (g.K - 1) / kt + 1 : 0;
-    const int64_t tiles = g.batches * a.mt * a.nt, steps = g.red * a.kt;
-    if (tiles < 256 && steps >= 8) {
-        const int64_t by_tiles = (512 + tiles - 1) / tiles, by_steps = steps / 4;
-        a.splits = (int32_t)(by_tiles < by_steps ? by_tiles : by_steps);
+    a.tile = 128;
+    for (;;) {
+        a.mt = (g.M - 1) / a.tile + 1;
+        a.nt = (g.N - 1) / (g.gated ? a.tile / 2 : a.tile) + 1;
+        // small tiles where large ones would leave CUs without work
+        if (a.tile == 64 || g.batches * a.mt * a.nt >= 512) break;
+        a.tile = 64;
     }
+    const int64_t tiles = g.batches * a.mt * a.nt, steps = g.red * a.kt;
+    int64_t splits = 1;
+    if (tiles < 512 && steps >= 8) splits = std::min((1024 + tiles - 1) / tiles, steps / 4);
+    a.per = steps ? (steps + splits - 1) / splits : 0;
+    a.splits = steps ? (int32_t)((steps + a.per - 1) / a.per) : 1;
     return a;
 }
+
+template <typename T, int TS>
+void launch_staged(const GemmArgs& a, unsigned grid, hipStream_t s)
+{
+    const Gemm& g = a.g;
+    if (g.gated) k_gemm<T, true, true, true, TS><<<grid, 256, 0, s>>>(a);
+    else if (g.a_kmajor && g.b_kmajor) k_gemm<T, true, true, false, TS><<<grid, 256, 0, s>>>(a);
+    else if (g.a_kmajor) k_gemm<T, true, false, false, TS><<<grid, 256, 0, s>>>(a);
+    else k_gemm<T, false, false, false, TS><<<grid, 256, 0, s>>>(a);
+}
+
+uint32_t join_quads(const Gemm& g) { return (uint32_t)(((int64_t)g.N + 3) / 4); }
 
 template <typename T>
 hipError_t launch_typed(const GemmArgs& a, hipStream_t s)
@@ -250,79 +321,123 @@ hipError_t launch_typed(const GemmArgs& a, hipStream_t s)
     const unsigned grid = (unsigned)(g.batches * a.splits * a.mt * a.nt);
     hipError_t e = hipSuccess;
     if (a.path == PATH_LARGE) e = launch_large(a, s);
-    else if (g.gated) k_gemm<T, true, true, true><<<grid, 256, 0, s>>>(a);
-    else if (g.a_kmajor && g.b_kmajor) k_gemm<T, true, true, false><<<grid, 256, 0, s>>>(a);
-    else if (g.a_kmajor) k_gemm<T, true, false, false><<<grid, 256, 0, s>>>(a);
-    else k_gemm<T, false, false, false><<<grid, 256, 0, s>>>(a);
+    else if (a.tile == 128) launch_staged<T, 128>(a, grid, s);
+    else launch_staged<T, 64>(a, grid, s);
     if (e == hipSuccess) e = hipGetLastError();
     if (e != hipSuccess || a.splits == 1) return e;
-    const unsigned join = (unsigned)((g.batches * g.M * g.N + 255) / 256);
-    if (g.gated) k_gemm_join<T, true><<<join, 256, 0, s>>>(a);
-    else k_gemm_join<T, false><<<join, 256, 0, s>>>(a);
+    const uint32_t quads = join_quads(g);
+    const int64_t total = g.batches * g.M * quads;
+    int32_t slices = 1;
+    while (slices < 16 && slices * 4 <= a.splits && total * slices < 131072) slices *= 2;
+    const unsigned join = (unsigned)((total * slices + 255) / 256);
+    if (g.gated) k_gemm_join<T, true><<<join, 256, 0, s>>>(a, total, quads, slices);
+    else k_gemm_join<T, false><<<join, 256, 0, s>>>(a, total, quads, slices);
     return hipGetLastError();
 }
 
 // ---- dz and its column sums -----------------------------------------------
-constexpr int Z_ROWS = 64;  // rows of a chunk
+// Bound by memory: dy and pre in, dz out.  A thread takes 16 bytes of a row and
+// every 2^(8 - lx)-th row of the chunk's 64, 2^lx threads side by side.
+constexpr int Z_ROWS = 64;
+
+struct GradZArgs {
+    GradZ g;
+    int64_t chunks;
+    uint32_t colblocks;
+    int32_t lx;
+    bool vec_dy, vec_pre;
+};
 
 template <typename T, bool GATED>
-__global__ __launch_bounds__(256) void k_gradz(GradZ g, int32_t colblocks, int64_t chunks)
+__global__ __launch_bounds__(256) void k_gradz(GradZArgs a)
 {
-    __shared__ float red[GATED ? 2 : 1][4][64];
+    constexpr int W = 16 / sizeof(T), NH = GATED ? 2 : 1;
     constexpr bool FAST = sizeof(T) == 2;
-    const int64_t wide = GATED ? 2 * (int64_t)g.out : g.out;
-    int64_t id = blockIdx.x;
-    const int32_t cb = (int32_t)(id % colblocks);
-    id /= colblocks;
-    const int64_t chunk = id % chunks, n = id / chunks;
-    const int32_t col = cb * 64 + threadIdx.x % 64;
-    const int part = threadIdx.x / 64;
-    float s0 = 0.f, s1 = 0.f;
-    if (col < g.out) {
-        for (int i = part; i < Z_ROWS; i += 4) {
-            const int64_t row = chunk * Z_ROWS + i;
-            if (row >= g.rows) break;
-            const float d = widen(static_cast<const T*>(g.dy)[n * g.dy_member + row * g.dy_row + col]);
-            const T* pre = static_cast<const T*>(g.pre) + n * g.pre_member + row * g.pre_row;
-            T* dz = static_cast<T*>(g.dz) + (n * g.rows + row) * g.ldz;
-            if constexpr (GATED) {
-                const float z = widen(pre[col]), u = widen(pre[g.out + col]);
-                const float dg = d * u * act_slope<FAST>(z, g.act), du = d * act_value<FAST>(z, g.act);
-                s0 += dg;
-                s1 += du;
-                if (g.dz) {
-                    dz[col] = (T)dg;
-                    dz[g.out + col] = (T)du;
+    __shared__ float red[NH][256 * W];
+    const GradZ& g = a.g;
+    const uint32_t cb = blockIdx.x % a.colblocks;
+    const int64_t outer = blockIdx.x / a.colblocks, chunk = outer % a.chunks, n = outer / a.chunks;
+    const int tx = threadIdx.x & ((1 << a.lx) - 1), ty = threadIdx.x >> a.lx, rows = 256 >> a.lx;
+    const int64_t col = (((int64_t)cb << a.lx) + tx) * W, left = g.out - col;
+    const T* dy = static_cast<const T*>(g.dy) + n * g.dy_member + col;
+    const T* pre = static_cast<const T*>(g.pre) + n * g.pre_member + col;
+    const int64_t row0 = chunk * Z_ROWS, end = g.rows - row0 < Z_ROWS ? g.rows - row0 : Z_ROWS;
+    float sum[NH][W];
+#pragma unroll
+    for (int h = 0; h < NH; ++h)
+#pragma unroll
+        for (int i = 0; i < W; ++i) sum[h][i] = 0.f;
+    if (left > 0) {
+        // one row at a time: more in flight cost the waves that hide the latency (2 rows 61 us against 60, 4 rows 84)
+        for (int r = ty; r < end; r += rows) {
+            const int64_t row = row0 + r;
+            float d[W], z[W], u[W], slope[W];
+            load_run<T, W>(dy + row * g.dy_row, a.vec_dy, left, d);
+            if (GATED || g.act != ES_ACT_NONE) {
+                load_run<T, W>(pre + row * g.pre_row, a.vec_pre, left, z);
+                if constexpr (GATED) load_run<T, W>(pre + row * g.pre_row + g.out, a.vec_pre, left, u);
+                activate<FAST, true, W>(g.act, z, slope);
+            }
+#pragma unroll
+            for (int i = 0; i < W; ++i) {
+                if constexpr (GATED) {
+                    u[i] *= d[i] * slope[i];
+                    d[i] *= z[i];
+                    sum[0][i] += u[i];
+                    sum[NH - 1][i] += d[i];
+                } else {
+                    if (g.act != ES_ACT_NONE) d[i] *= slope[i];
+                    sum[0][i] += d[i];
                 }
-            } else {
-                const float dd = g.act == ES_ACT_NONE ? d : d * act_slope<FAST>(widen(pre[col]), g.act);
-                s0 += dd;
-                if (g.dz) dz[col] = (T)dd;
+            }
+            if (g.dz) {
+                // rows of whole pieces; a gated layer's second half may start within one
+                T* dz = static_cast<T*>(g.dz) + (n * g.rows + row) * g.ldz + col;
+                store_run<T, W>(dz, true, left, GATED ? u : d);
+                if constexpr (GATED) store_run<T, W>(dz + g.out, g.out % W == 0, left, d);
             }
         }
     }
-    if (!g.sums) return;
-    red[0][part][threadIdx.x % 64] = s0;
-    if constexpr (GATED) red[GATED][part][threadIdx.x % 64] = s1;
+    if (!g.sums && !g.db) return;
+#pragma unroll
+    for (int h = 0; h < NH; ++h)
+#pragma unroll
+        for (int i = 0; i < W; ++i) red[h][(ty * W + i) * (1 << a.lx) + tx] = sum[h][i];
     __syncthreads();
-    if (part == 0 && col < g.out) {
-        float* out = g.sums + (n * chunks + chunk) * wide;
-        const int c = threadIdx.x % 64;
-        out[col] = (red[0][0][c] + red[0][1][c]) + (red[0][2][c] + red[0][3][c]);
-        if constexpr (GATED)
-            out[g.out + col] = (red[GATED][0][c] + red[GATED][1][c]) + (red[GATED][2][c] + red[GATED][3][c]);
+    // a column's rows in their order
+    const int cols = W << a.lx;
+    const int64_t wide = NH * (int64_t)g.out;
+    for (int c = threadIdx.x; c < cols; c += 256) {
+        const int64_t o = ((int64_t)cb << a.lx) * W + c;
+        if (o >= g.out) break;
+        const int at = (c % W) * (1 << a.lx) + c / W;
+#pragma unroll
+        for (int h = 0; h < NH; ++h) {
+            float s = 0.f;
+            for (int r = 0; r < rows; ++r) s += red[h][r * cols + at];
+            if (g.db) static_cast<T*>(g.db)[n * g.db_member + h * g.out + o] = (T)s;
+            else g.sums[(n * a.chunks + chunk) * wide + h * g.out + o] = s;
+        }
     }
 }
 
+// 16 columns side by side, blockDim.x / 16 slices of the chunks, each in its order
 template <typename T>
-__global__ __launch_bounds__(256) void k_bias_grad(const float* sums, int64_t members, int64_t chunks, int64_t wide, T* db,
-                                                   int64_t db_member, int64_t groups)
+__global__ __launch_bounds__(1024) void k_bias_grad(const float* sums, int64_t count, int64_t wide, T* db, int64_t db_member,
+                                                    uint32_t colblocks)
 {
-    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (id >= groups * wide) return;
-    const int64_t n = id / wide, o = id % wide, count = chunks * members / groups;
+    __shared__ double red[1024];
+    const int64_t n = blockIdx.x / colblocks, o = (int64_t)(blockIdx.x % colblocks) * 16 + threadIdx.x % 16;
+    const int slice = threadIdx.x / 16, slices = blockDim.x / 16;
     double s = 0.0;
-    for (int64_t c = 0; c < count; ++c) s += (double)sums[(n * count + c) * wide + o];
+    if (o < wide) {
+#pragma unroll 4
+        for (int64_t c = slice; c < count; c += slices) s += (double)sums[(n * count + c) * wide + o];
+    }
+    red[threadIdx.x] = s;
+    __syncthreads();
+    if (slice || o >= wide) return;
+    for (int i = 1; i < slices; ++i) s += red[threadIdx.x + 16 * i];
     db[n * db_member + o] = (T)(float)s;
 }
 
@@ -340,7 +455,7 @@ bool gemm_too_large(const Gemm& g)
     const __int128 most = 0x7FFFFFFF;
     if (a.path == PATH_ROWS) return (__int128)g.batches * a.nt > most;
     return (__int128)g.batches * a.splits * a.mt * a.nt > most ||
-           (a.splits > 1 && (__int128)g.batches * g.M * g.N / 256 >= most);
+           (a.splits > 1 && (__int128)g.batches * g.M * join_quads(g) / 256 >= most);
 }
 
 hipError_t launch_gemm(const Gemm& g, float* partial, hipStream_t s)
@@ -356,13 +471,28 @@ hipError_t launch_gemm(const Gemm& g, float* partial, hipStream_t s)
 
 int64_t gradz_chunks(int64_t rows) { return (rows + Z_ROWS - 1) / Z_ROWS; }
 
+__int128 gradz_workgroups(const GradZ& g)
+{
+    const int64_t pieces = ((int64_t)g.out * dtype_size(g.dtype) + 15) / 16;
+    int lx = 0;
+    while (lx < 5 && (int64_t)1 << lx < pieces) ++lx;
+    return (__int128)g.members * gradz_chunks(g.rows) * ((pieces + (1 << lx) - 1) >> lx);
+}
+
 hipError_t launch_gradz(const GradZ& g, hipStream_t s)
 {
-    const int64_t chunks = gradz_chunks(g.rows);
-    const int32_t colblocks = (g.out + 63) / 64;
-    const int64_t grid = g.members * chunks * colblocks;
+    GradZArgs a{};
+    a.g = g;
+    a.chunks = gradz_chunks(g.rows);
+    const size_t e = dtype_size(g.dtype);
+    const int64_t pieces = ((int64_t)g.out * e + 15) / 16;
+    while (a.lx < 5 && (int64_t)1 << a.lx < pieces) ++a.lx;
+    a.colblocks = (uint32_t)((pieces + (1 << a.lx) - 1) >> a.lx);
+    a.vec_dy = whole(g.dy, g.dy_row, g.dy_member, g.rows, g.members, e);
+    a.vec_pre = whole(g.pre, g.pre_row, g.pre_member, g.rows, g.members, e) && (!g.gated || g.out * e % 16 == 0);
+    const int64_t grid = g.members * a.chunks * a.colblocks;
     if (grid == 0) return hipSuccess;
-    auto go = [&](auto kernel) { kernel<<<(unsigned)grid, 256, 0, s>>>(g, colblocks, chunks); };
+    auto go = [&](auto kernel) { kernel<<<(unsigned)grid, 256, 0, s>>>(a); };
     switch (g.dtype) {
     case ES_BF16: g.gated ? go(k_gradz<__bf16, true>) : go(k_gradz<__bf16, false>); break;
     case ES_F16: g.gated ? go(k_gradz<_Float16, true>) : go(k_gradz<_Float16, false>); break;
@@ -371,19 +501,18 @@ hipError_t launch_gradz(const GradZ& g, hipStream_t s)
     return hipGetLastError();
 }
 
-hipError_t launch_bias_grad(int32_t dtype, const float* sums, int64_t members, int64_t chunks, int64_t wide, void* db,
+hipError_t launch_bias_grad(int32_t dtype, const float* sums, int64_t groups, int64_t count, int64_t wide, void* db,
                             int64_t db_member, hipStream_t s)
 {
-    const int64_t groups = members != 1 && db_member == 0 ? 1 : members;
-    const unsigned grid = (unsigned)((groups * wide + 255) / 256);
+    const uint32_t colblocks = (uint32_t)((wide + 15) / 16);
+    unsigned threads = 64;
+    while (threads < 1024 && threads / 16 < count) threads *= 2;
+    const unsigned grid = (unsigned)(groups * colblocks);
+    auto go = [&](auto* out) { k_bias_grad<<<grid, threads, 0, s>>>(sums, count, wide, out, db_member, colblocks); };
     switch (dtype) {
-    case ES_BF16:
-        k_bias_grad<<<grid, 256, 0, s>>>(sums, members, chunks, wide, static_cast<__bf16*>(db), db_member, groups);
-        break;
-    case ES_F16:
-        k_bias_grad<<<grid, 256, 0, s>>>(sums, members, chunks, wide, static_cast<_Float16*>(db), db_member, groups);
-        break;
-    default: k_bias_grad<<<grid, 256, 0, s>>>(sums, members, chunks, wide, static_cast<float*>(db), db_member, groups);
+    case ES_BF16: go(static_cast<__bf16*>(db)); break;
+    case ES_F16: go(static_cast<_Float16*>(db)); break;
+    default: go(static_cast<float*>(db));
     }
     return hipGetLastError();
 }

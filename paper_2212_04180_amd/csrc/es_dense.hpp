@@ -55,11 +55,14 @@ struct GradZ {
     void* dz;  // null: not stored
     int64_t ldz;
     float* sums;  // [members][chunks][wide], null: not wanted
+    void* db;     // with one chunk of rows a member: where its sums go instead, in the type; null: to sums
+    int64_t db_member;
 };
 int64_t gradz_chunks(int64_t rows);
+__int128 gradz_workgroups(const GradZ& g);
 hipError_t launch_gradz(const GradZ& g, hipStream_t s);
-// db[n][o] (db_member 0: summed over the members) from the chunks' sums
-hipError_t launch_bias_grad(int32_t dtype, const float* sums, int64_t members, int64_t chunks, int64_t wide, void* db,
+// db[n][o], n < groups, from [groups][count][wide] sums
+hipError_t launch_bias_grad(int32_t dtype, const float* sums, int64_t groups, int64_t count, int64_t wide, void* db,
                             int64_t db_member, hipStream_t s);
 
 }  // namespace esmi

@@ -12,9 +12,11 @@
 // The loads write LDS in lane order, so the spreading over its banks is done by
 // which 16 bytes a lane fetches:
 //   k-major operand (k contiguous): 64 bytes of k a row; piece c of row r lies at
-//     position c ^ f(r), f(r) the two bits of r in which the four groups of
-//     rows of a fragment differ (2-3, or 4-5 and 3-4 on the n side): the reads of
-//     16 lanes cover all banks;
+//     position c ^ f(r).  A 16-byte read serves lanes {0-3, 12-15, 20-27},
+//     {4-11, 16-19, 28-31} and those + 32 together (measured), so the rows 4-11 of
+//     a fragment meet the other rows' next piece: f is 3 for its upper 8 rows,
+//     which spreads each such 16 over all banks (any f that spreads 16 lanes in
+//     a row costs twice the cycles);
 //   else: a row of m (n) per k, read back transposed by ds_read_b64_tr_b16, which
 //     hands lane i of 16 the four k of column i.
 // Rows, columns and k beyond the matrices are not fetched: a buffer load out of
@@ -28,22 +30,30 @@ namespace esmi {
 
 namespace {
 
-constexpr int BM = 256, BN = 128, BK = 32, STAGES = 3;
+constexpr int BM = 256, BN = 128, BK = 32, STAGES = 3;  // k_gemm_large
 constexpr int A_BYTES = BM * BK * 2, B_BYTES = BN * BK * 2, STAGE_BYTES = A_BYTES + B_BYTES;
 constexpr uint32_t OUT = 0x80000000u;  // an offset beyond every buffer's range
 
 typedef __attribute__((address_space(3))) void lds_void;
 typedef short shortx4 __attribute__((ext_vector_type(4)));
 
-// One operand's share of a step: EXT rows (k-major) or columns.
-// SHIFT: the lower of the two row bits that spread a k-major fragment's rows.
-template <bool KMAJOR, bool PERM, int EXT, int SHIFT>
+// One operand's share of a step of STEP k: EXT rows (k-major) or columns,
+// fetched by THREADS threads.
+template <bool KMAJOR, int EXT, int STEP, int THREADS>
 struct Operand {
-    static constexpr int LOADS = EXT * BK * 2 / (256 * 16);  // per lane
-    static constexpr int ROW = EXT * 2;                      // bytes of a k row (not k-major)
+    static constexpr int LOADS = EXT * STEP * 2 / (THREADS * 16);  // per lane
+    static constexpr int ROW = KMAJOR ? STEP * 2 : EXT * 2;        // bytes of a staged row
+    static constexpr int PIECES = ROW / 16;
     uint32_t off[LOADS];
 
-    static __device__ __forceinline__ int f(int r) { return (r >> SHIFT) & 3; }
+    static __device__ __forceinline__ int f(int r)
+    {
+        const int a = (r >> 2) & 3;
+        if constexpr (STEP == 32) return 3 * (a >> 1);
+        return (2 * a + ((r >> 1) & 1)) ^ ((a ^ (a >> 1)) & 1);
+    }
+    // pairs of pieces (16 columns) of different k rows on different banks
+    static __device__ __forceinline__ int spread(int k) { return 2 * ((k & 3) | ((k >> 1) & 4)); }
 
     // row_of(i): the matrix's row (k-major) or first column of the staged piece i, -1 if outside
     template <typename F>
@@ -51,53 +61,50 @@ struct Operand {
     {
 #pragma unroll
         for (int j = 0; j < LOADS; ++j) {
-            const int p = (int)threadIdx.x + 256 * j;  // 16-byte piece of the stage
+            const int p = (int)threadIdx.x + THREADS * j;  // 16-byte piece of the stage
             if constexpr (KMAJOR) {
-                const int r = p / 4, c = (p % 4) ^ f(r);
+                const int r = p / PIECES, c = (p % PIECES) ^ f(r);
                 const int64_t row = row_of(r);
                 off[j] = row >= 0 ? (uint32_t)((row * stride + 8 * c) * 2) : OUT;
             } else {
-                const int k = p / (ROW / 16), c = (p % (ROW / 16)) ^ spread(k);
+                const int k = p / PIECES, c = (p % PIECES) ^ spread(k);
                 const int64_t col = row_of(8 * c);
                 off[j] = col >= 0 ? (uint32_t)((k * stride + col) * 2) : OUT;
             }
         }
     }
-    // pairs of 16-byte pieces (16 columns) of different k rows on different banks
-    static __device__ __forceinline__ int spread(int k) { return 2 * ((k & 3) | ((k >> 1) & 4)); }
 
-    // the step at k0, base: the tile's first row at k0 (k-major) or k row k0
+    // Piece j of the step at k0, base: the tile's first row at k0 (k-major) or k
+    // row k0.  A lane's pieces all lie at the same k of their rows (k-major).
+    __device__ __forceinline__ void load(int j, const void* base, int64_t stride, int32_t k_left, unsigned char* lds) const
+    {
+        static_assert(!KMAJOR || THREADS / PIECES % 16 == 0, "f() is the same for all pieces of a lane");
+        const int64_t range = KMAJOR ? 0x7FFFFFFF : (k_left < STEP ? k_left : STEP) * stride * 2;
+        auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, (int)range, 0x00020000);
+        const int p = (int)threadIdx.x, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+        const bool inside = !KMAJOR || 8 * ((p % PIECES) ^ f(p / PIECES)) < k_left;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void*)(lds + (THREADS * j + 64 * wave) * 16), 16,
+                                                 (int)(inside ? off[j] : OUT), 0, 0, 0);
+    }
     __device__ __forceinline__ void fetch(const void* base, int64_t stride, int32_t k_left, unsigned char* lds) const
     {
-        const int64_t range = KMAJOR ? 0x7FFFFFFF : (k_left < BK ? k_left : BK) * stride * 2;
-        auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, (int)range, 0x00020000);
-        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
 #pragma unroll
-        for (int j = 0; j < LOADS; ++j) {
-            uint32_t o = off[j];
-            if constexpr (KMAJOR) {
-                if (k_left < BK) {
-                    const int p = (int)threadIdx.x + 256 * j;
-                    if (8 * ((p % 4) ^ f(p / 4)) >= k_left) o = OUT;
-                }
-            }
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_void*)(lds + (256 * j + 64 * wave) * 16), 16, (int)o, 0, 0, 0);
-        }
+        for (int j = 0; j < LOADS; ++j) load(j, base, stride, k_left, lds);
     }
 
-    // the fragment of staged rows / columns base + slot(l16) (PERM: tile b of 64)
-    __device__ __forceinline__ uintx4 read(const unsigned char* lds, int base, int b, int lane) const
+    // the fragment of 32 k, the `ks`th, of staged rows (columns) base + 16 b + l16
+    static __device__ __forceinline__ uintx4 read(const unsigned char* lds, int base, int b, int ks, int lane)
     {
         const int l16 = lane % 16, q = lane / 16;
         if constexpr (KMAJOR) {
-            const int r = PERM ? base + 16 * (l16 >> 2) + 4 * b + (l16 & 3) : base + 16 * b + l16;
-            return *reinterpret_cast<const uintx4*>(lds + r * 64 + ((q ^ f(r)) * 16));
+            const int row = base + 16 * b + l16;
+            return *reinterpret_cast<const uintx4*>(lds + row * ROW + ((4 * ks + q) ^ f(row)) * 16);
         } else {
             const int col = base + 16 * b + 4 * (l16 & 3);
             shortx4 v[2];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const int k = 8 * q + 4 * h + (l16 >> 2);
+                const int k = 32 * ks + 8 * q + 4 * h + (l16 >> 2);
                 const unsigned char* p = lds + k * ROW + (((col / 8) ^ spread(k)) * 16) + (col % 8) * 2;
                 v[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) shortx4*)p);
             }
@@ -126,23 +133,24 @@ __global__ __launch_bounds__(256, 2) void k_gemm_large(GemmArgs a)
     extern __shared__ __align__(1024) unsigned char lds[];
     const Gemm& g = a.g;
     constexpr int OUTS = GATED ? BN / 2 : BN;  // outputs of a tile
-    constexpr bool PERM = BKM && !GATED;
     const uint32_t tiles = (uint32_t)a.mt * a.nt, outer = blockIdx.x / tiles;
     int32_t tm, tn;
     tile_of(blockIdx.x % tiles, a.mt, a.nt, tm, tn);
     const int32_t split = __builtin_amdgcn_readfirstlane(outer % a.splits);
     const int64_t batch = (uint32_t)__builtin_amdgcn_readfirstlane(outer / a.splits);
     const int32_t m0 = tm * BM, n0 = tn * OUTS;
-    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), q = lane / 16, l16 = lane % 16;
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int wm = wave / 2, wn = wave % 2;
     const int32_t steps = (int32_t)g.red * a.kt;  // below 2^31
-    const int32_t first = split * a.per, last = steps - first < a.per ? steps : first + a.per;
+    const int32_t per = (int32_t)a.per, first = split * per, last = steps - first < per ? steps : first + per;
 
     // bases at the tile's first row (k-major) or column
     const T* A = static_cast<const T*>(g.a) + batch * g.a_batch + (AK ? m0 * g.a_row : 0);
     const T* B = static_cast<const T*>(g.b) + batch * g.b_batch + (BKM && !GATED ? n0 * g.b_row : 0);
-    Operand<AK, false, BM, 2> oa;
-    Operand<BKM, PERM, BN, GATED ? 3 : PERM ? 4 : 2> ob;
+    using OA = Operand<AK, BM, BK, 256>;
+    using OB = Operand<BKM, BN, BK, 256>;
+    OA oa;
+    OB ob;
     oa.init(g.a_row, [&](int i) -> int64_t { return m0 + i < g.M ? (AK ? i : m0 + i) : -1; });
     if constexpr (GATED) {
         // 32 gates, then their 32 others, for each wave's 64
@@ -181,7 +189,7 @@ __global__ __launch_bounds__(256, 2) void k_gemm_large(GemmArgs a)
             pb += g.b_red;
         }
     };
-    static_assert(oa.LOADS + ob.LOADS == 6, "loads per step, counted below");
+    static_assert(OA::LOADS + OB::LOADS == 6, "loads per step, counted below");
     fetch(first);
     fetch(first + 1);
     for (int32_t t = first; t < last; ++t) {
@@ -196,65 +204,199 @@ __global__ __launch_bounds__(256, 2) void k_gemm_large(GemmArgs a)
         from = from == (STAGES - 1) * STAGE_BYTES ? 0 : from + STAGE_BYTES;
         uintx4 fb[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            if constexpr (GATED) {
-                const int row = 64 * wn + 32 * (j >> 1) + 8 * (l16 >> 2) + 4 * (j & 1) + (l16 & 3);
-                fb[j] = *reinterpret_cast<const uintx4*>(now + A_BYTES + row * 64 + ((q ^ ob.f(row)) * 16));
-            } else {
-                fb[j] = ob.read(now + A_BYTES, 64 * wn, j, lane);
-            }
-        }
+        for (int j = 0; j < 4; ++j) fb[j] = OB::read(now + A_BYTES, 64 * wn, j, 0, lane);
+        uintx4 fa[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const uintx4 fa = oa.read(now, 128 * wm, i, lane);
+        for (int i = 0; i < 8; ++i) fa[i] = OA::read(now, 128 * wm, i, 0, lane);
+        // all reads under way before the first product: left to itself the compiler
+        // reads two fragments at a time and waits for each
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) acc[i][j] = product<T>(fb[j], fa, acc[i][j]);
-        }
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[i][j] = product<T>(fb[j], fa[i], acc[i][j]);
     }
 
-    // a lane's outputs of a row: 16 in a row, 8 of a gated layer, or four times 4
-    constexpr int W = GATED ? 8 : PERM ? 16 : 4;
+    __syncthreads();  // the buffers serve the epilogue
+    epilogue<T, GATED, 8, 4>(a, split, batch, m0 + 128 * wm, n0 + (GATED ? 32 : 64) * wn, acc,
+                             reinterpret_cast<float*>(lds + wave * EPILOGUE_LDS<4>), lane);
+}
+static_assert(4 * EPILOGUE_LDS<4> <= STAGES * STAGE_BYTES, "the epilogue's rows fit the buffers");
+
+// 256 x 256 tiles for products that fill the chip with them.  Eight waves, 128 x
+// 64 each, in two groups of one wave a SIMD, half a step of 32 k apart: while
+// one group multiplies (32 products, 512 cycles) and issues loads in between, the
+// other reads its next fragments; a barrier ends each such phase.  A step is 64
+// k: whole 128-byte lines of a k-major operand.  Two buffers of 64 KB; the loads
+// of step t + 1 are issued once both groups have read step t - 1:
+//   phase     4t        4t + 1    4t + 2   4t + 3   4t + 4
+//   group 0   read 0    mul 0, l  read 1   mul 1    read 0 of t + 1
+//   group 1   mul 1, l  read 0    mul 0    read 1   mul 1, l
+//   (l: loads of t + 1, all there after 4t + 3)
+// 8192 x 4096 x 4096 bf16 209 us, 1315 TFLOP/s; the products alone take 138, with
+// the fragments' reads 155, the loads alone 137: reads and loads share the LDS.
+constexpr int WT = 256, WK = 64, W_BYTES = WT * WK * 2;  // of one operand's buffer
+
+template <typename T, bool AK, bool BKM, bool GATED>
+__global__ __launch_bounds__(512, 2) void k_gemm_wide(GemmArgs a)
+{
+    extern __shared__ __align__(1024) unsigned char lds[];
+    const Gemm& g = a.g;
+    constexpr int OUTS = GATED ? WT / 2 : WT;
+    const uint32_t tiles = (uint32_t)a.mt * a.nt, outer = blockIdx.x / tiles;
+    int32_t tm, tn;
+    tile_of(blockIdx.x % tiles, a.mt, a.nt, tm, tn);
+    const int32_t split = __builtin_amdgcn_readfirstlane(outer % a.splits);
+    const int64_t batch = (uint32_t)__builtin_amdgcn_readfirstlane(outer / a.splits);
+    const int32_t m0 = tm * WT, n0 = tn * OUTS;
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64); const int group = wave / 4, wm = group, wn = wave % 4;
+    const int32_t steps = (int32_t)g.red * a.kt;  // below 2^31
+    const int32_t per = (int32_t)a.per, first = split * per, count = steps - first < per ? steps - first : per;
+
+    using OA = Operand<AK, WT, WK, 512>;
+    using OB = Operand<BKM, WT, WK, 512>;
+    OA oa;
+    OB ob;
+    const T* pa = static_cast<const T*>(g.a) + batch * g.a_batch + (AK ? m0 * g.a_row : 0);
+    const T* pb = static_cast<const T*>(g.b) + batch * g.b_batch + (BKM && !GATED ? n0 * g.b_row : 0);
+    oa.init(g.a_row, [&](int i) -> int64_t { return m0 + i < g.M ? (AK ? i : m0 + i) : -1; });
+    if constexpr (GATED) {
+        ob.init(g.b_row, [&](int i) -> int64_t {
+            const int32_t n = n0 + 32 * (i / 64) + i % 32;
+            return n < g.N ? n + (i / 32 % 2 ? (int64_t)g.N : 0) : -1;
+        });
+    } else {
+        ob.init(g.b_row, [&](int i) -> int64_t { return n0 + i < g.N ? (BKM ? i : n0 + i) : -1; });
+    }
+    int32_t kt = first;
+    if (a.splits > 1 && g.red > 1) {
+        const int32_t r = __builtin_amdgcn_readfirstlane((uint32_t)first / (uint32_t)a.kt);
+        kt = first - r * a.kt;
+        pa += r * g.a_red;
+        pb += r * g.b_red;
+    }
+    auto fetch = [&](int32_t t) {  // step t of this workgroup's; behind the last one nothing is fetched
+        const int32_t k0 = kt * WK, left = t < count ? g.K - k0 : 0;
+        unsigned char* to = lds + (t & 1) * 2 * W_BYTES;
+        oa.fetch(pa + (AK ? (int64_t)k0 : k0 * g.a_row), g.a_row, left, to);
+        ob.fetch(pb + (BKM ? (int64_t)k0 : k0 * g.b_row), g.b_row, left, to + W_BYTES);
+        if (++kt == a.kt) {
+            kt = 0;
+            pa += g.a_red;
+            pb += g.b_red;
+        }
+    };
+
+    floatx4 acc[8][4];  // [m tile][n tile]
 #pragma unroll
-    for (int p = 0; p < (W == 4 ? 4 : 1); ++p) {
-        const int64_t n = GATED ? n0 + 32 * wn + 8 * q : PERM ? n0 + 64 * wn + 16 * q : n0 + 64 * wn + 16 * p + 4 * q;
-        float bz[W], bu[W];
-        load_bias<T, GATED, W>(g, batch, n, bz, bu);
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+    uintx4 fa[8], fb[4];
+    auto read = [&](int32_t t, int ks) {
+        const unsigned char* from = lds + (t & 1) * 2 * W_BYTES;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) fb[j] = OB::read(from + W_BYTES, 64 * wn, j, ks, lane);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) fa[i] = OA::read(from, 128 * wm, i, ks, lane);
+    };
+    auto multiply = [&]() {
+        __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[i][j] = product<T>(fb[j], fa[i], acc[i][j]);
+        __builtin_amdgcn_s_setprio(0);
+    };
+    // the same with the loads of step t in between
+    auto multiply_fetch = [&](int32_t t) {
+        const int32_t k0 = kt * WK, left = t < count ? g.K - k0 : 0;
+        unsigned char* to = lds + (t & 1) * 2 * W_BYTES;
+        const T* ba = pa + (AK ? (int64_t)k0 : k0 * g.a_row);
+        const T* bb = pb + (BKM ? (int64_t)k0 : k0 * g.b_row);
+        if (++kt == a.kt) {
+            kt = 0;
+            pa += g.a_red;
+            pb += g.b_red;
+        }
+        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const int64_t m = m0 + 128 * wm + 16 * i + l16;
-            if (m >= g.M) continue;
-            float z[W], u[W];
+            if (i % 2 == 0) oa.load(i / 2, ba, g.a_row, left, to);
+            else ob.load(i / 2, bb, g.b_row, left, to + W_BYTES);
 #pragma unroll
-            for (int e = 0; e < W; ++e) {
-                z[e] = acc[i][p + e / 4][e % 4];
-                u[e] = GATED ? acc[i][(e / 4 + 2) % 4][e % 4] : 0.f;
-            }
-            if (a.splits > 1) store_partial<GATED, W>(a, split, batch, m, n, z, u);
-            else {
-                float r[W];
-                load_res<T, W>(a, batch, m, n, r);
-                finish<T, GATED, W>(a, batch, m, n, z, u, bz, bu, r);
-            }
+            for (int j = 0; j < 4; ++j) acc[i][j] = product<T>(fb[j], fa[i], acc[i][j]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        __builtin_amdgcn_s_setprio(0);
+    };
+    // ends a phase: what this wave has read is in its registers
+    auto phase = [&]() {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("" ::: "memory");
+    };
+    auto arrived = [&]() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); };
+
+    fetch(0);
+    arrived();
+    phase();
+    if (group == 0) {
+        for (int32_t t = 0; t < count; ++t) {
+            read(t, 0);
+            phase();
+            multiply_fetch(t + 1);
+            phase();
+            read(t, 1);
+            phase();
+            multiply();
+            arrived();
+            phase();
+        }
+        phase();
+    } else {
+        fetch(1);
+        phase();
+        for (int32_t t = 0; t < count; ++t) {
+            read(t, 0);
+            phase();
+            multiply();
+            phase();
+            read(t, 1);
+            arrived();
+            phase();
+            multiply_fetch(t + 2);
+            phase();
         }
     }
+    arrived();
+    __syncthreads();  // the buffers serve the epilogue
+    epilogue<T, GATED, 8, 4>(a, split, batch, m0 + 128 * wm, n0 + (GATED ? 32 : 64) * wn, acc,
+                             reinterpret_cast<float*>(lds + wave * EPILOGUE_LDS<4>), lane);
 }
+static_assert(8 * EPILOGUE_LDS<4> <= 4 * W_BYTES, "the epilogue's rows fit the buffers");
 
 template <typename T>
 hipError_t launch_typed(const GemmArgs& a, hipStream_t s)
 {
     const Gemm& g = a.g;
     const unsigned grid = (unsigned)(g.batches * a.splits * a.mt * a.nt);
-    auto go = [&](void (*kernel)(GemmArgs)) {
+    const bool wide = a.tile == WT;
+    auto go = [&](void (*large)(GemmArgs), void (*wider)(GemmArgs)) {
+        void (*kernel)(GemmArgs) = wide ? wider : large;
+        const int bytes = wide ? 4 * W_BYTES : STAGES * STAGE_BYTES;
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize,
-                                                 STAGES * STAGE_BYTES);
+                                                 bytes);
         if (e != hipSuccess) return e;
-        kernel<<<grid, 256, STAGES * STAGE_BYTES, s>>>(a);
+        kernel<<<grid, wide ? 512 : 256, bytes, s>>>(a);
         return hipGetLastError();
     };
-    if (g.gated) return go(k_gemm_large<T, true, true, true>);
-    if (g.a_kmajor && g.b_kmajor) return go(k_gemm_large<T, true, true, false>);
-    if (g.a_kmajor) return go(k_gemm_large<T, true, false, false>);
-    return go(k_gemm_large<T, false, false, false>);
+    if (g.gated) return go(k_gemm_large<T, true, true, true>, k_gemm_wide<T, true, true, true>);
+    if (g.a_kmajor && g.b_kmajor) return go(k_gemm_large<T, true, true, false>, k_gemm_wide<T, true, true, false>);
+    if (g.a_kmajor) return go(k_gemm_large<T, true, false, false>, k_gemm_wide<T, true, false, false>);
+    return go(k_gemm_large<T, false, false, false>, k_gemm_wide<T, false, false, false>);
 }
 
 bool pieces(const Gemm& g, const void* p, int64_t row, int64_t batch, int64_t red)
@@ -277,9 +419,9 @@ bool large_fits(const Gemm& g)
     // the buffers' ranges end k rows: these lie behind each other
     if ((!g.a_kmajor && g.a_row < g.M) || (!g.b_kmajor && g.b_row < g.N)) return false;
     const int64_t reach = (int64_t)1 << 30;
-    if ((g.a_kmajor ? BM : BK) * g.a_row * 2 + (g.a_kmajor ? 0 : (int64_t)g.M * 2) > reach) return false;
+    if ((g.a_kmajor ? WT : WK) * g.a_row * 2 + (g.a_kmajor ? 0 : (int64_t)g.M * 2) > reach) return false;
     // a gated layer's two halves lie N rows apart
-    if ((g.b_kmajor ? BN + (g.gated ? 2 * (int64_t)g.N : 0) : BK) * g.b_row * 2 + (g.b_kmajor ? 0 : (int64_t)g.N * 2) > reach) return false;
+    if ((g.b_kmajor ? WT + (g.gated ? 2 * (int64_t)g.N : 0) : WK) * g.b_row * 2 + (g.b_kmajor ? 0 : (int64_t)g.N * 2) > reach) return false;
     return g.M >= 64 && g.N >= 64;
 }
 
@@ -287,15 +429,24 @@ void large_plan(GemmArgs& a)
 {
     const Gemm& g = a.g;
     a.path = PATH_LARGE;
-    a.mt = (g.M - 1) / BM + 1;
-    a.nt = (g.N - 1) / (g.gated ? BN / 2 : BN) + 1;
-    a.kt = (g.K - 1) / BK + 1;
-    const int64_t tiles = g.batches * a.mt * a.nt, steps = g.red * a.kt;
-    if (tiles < 384 && steps >= 16) {
-        const int64_t by_tiles = (512 + tiles - 1) / tiles, by_steps = steps / 8;
-        a.splits = (int32_t)(by_tiles < by_steps ? by_tiles : by_steps);
+    a.tile = WT;
+    a.mt = (g.M - 1) / WT + 1;
+    a.nt = (g.N - 1) / (g.gated ? WT / 2 : WT) + 1;
+    a.kt = (g.K - 1) / WK + 1;
+    int64_t tiles = g.batches * a.mt * a.nt, steps = g.red * a.kt;
+    if (tiles < 192) {
+        a.tile = BN;
+        a.mt = (g.M - 1) / BM + 1;
+        a.nt = (g.N - 1) / (g.gated ? BN / 2 : BN) + 1;
+        a.kt = (g.K - 1) / BK + 1;
+        tiles = g.batches * a.mt * a.nt;
+        steps = g.red * a.kt;
+        if (tiles < 384 && steps >= 16) {
+            const int64_t by_tiles = (512 + tiles - 1) / tiles, by_steps = steps / 8;
+            a.splits = (int32_t)(by_tiles < by_steps ? by_tiles : by_steps);
+        }
     }
-    a.per = (int32_t)((steps + a.splits - 1) / a.splits);
+    a.per = (steps + a.splits - 1) / a.splits;
     a.splits = (int32_t)((steps + a.per - 1) / a.per);
 }
 

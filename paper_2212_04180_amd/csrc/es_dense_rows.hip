@@ -76,7 +76,7 @@ __global__ __launch_bounds__(64 * MOST_WAVES) void k_rows(GemmArgs a)
         for (int i = 0; i < MT; ++i) load_res<T, 4>(a, batch, 16 * i + l16 < g.M ? 16 * i + l16 : g.M - 1, o, r[i]);
     }
 
-    const int32_t c0 = part * a.per, c1 = a.kt - c0 < a.per ? a.kt : c0 + a.per, full = g.K / CHUNK < c1 ? g.K / CHUNK : c1;
+    const int32_t per = (int32_t)a.per, c0 = part * per, c1 = a.kt - c0 < per ? a.kt : c0 + per, full = g.K / CHUNK < c1 ? g.K / CHUNK : c1;
     int32_t c = c0;
     int64_t at = (int64_t)c0 * CHUNK + E * q;
     auto batch_of = [&](auto count) {

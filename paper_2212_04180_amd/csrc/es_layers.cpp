@@ -153,6 +153,7 @@ struct BackwardPlan {
     GradZ z;
     Gemm dx, dw;
     bool do_dx, do_dw, do_db, store_dz;
+    bool db_there;  // each db is one chunk's sums: no second launch
     int64_t wide, chunks;
     size_t dz_bytes, sums_bytes, partial_bytes;
     size_t total() const { return dz_bytes + sums_bytes + partial_bytes; }
@@ -172,7 +173,8 @@ BackwardPlan plan_backward(const es_dense_grad_args& a, bool gated)
     p.chunks = gradz_chunks(B);
     const int64_t ldz = (wide + 7) / 8 * 8;  // whole 16-byte pieces in every type
     p.dz_bytes = p.store_dz ? up((size_t)n * B * ldz * e) : 0;
-    p.sums_bytes = p.do_db ? up((size_t)n * p.chunks * wide * 4) : 0;
+    p.db_there = p.do_db && p.chunks == 1 && !sum_db;
+    p.sums_bytes = p.do_db && !p.db_there ? up((size_t)n * p.chunks * wide * 4) : 0;
     p.z.dtype = a.dtype; p.z.act = a.act; p.z.gated = gated;
     p.z.members = n; p.z.rows = (int32_t)B; p.z.out = (int32_t)a.out;
     p.z.dy = a.dy.p; p.z.dy_member = a.dy.member; p.z.dy_row = a.dy.row;
@@ -228,7 +230,7 @@ es_status backward(const es_dense_grad_args* a, bool gated, const char* who, voi
     if (backward_bad(*a, gated, c)) return refuse(c);
     BackwardPlan p = plan_backward(*a, gated);
     if ((p.do_dx && gemm_too_large(p.dx)) || (p.do_dw && gemm_too_large(p.dw)) ||
-        (__int128)a->members * p.chunks * ((p.wide + 63) / 64) > kMaxDim)
+        gradz_workgroups(p.z) > kMaxDim || (__int128)a->members * ((p.wide + 15) / 16) > kMaxDim)
         return init_fail(ES_ERR_UNSUPPORTED, "more workgroups than a launch holds", who);
     const size_t want = p.total();
     if (need) {
@@ -240,15 +242,23 @@ es_status backward(const es_dense_grad_args* a, bool gated, const char* who, voi
     char* at = static_cast<char*>(ws);
     hipStream_t s = static_cast<hipStream_t>(stream);
     hipError_t e = hipSuccess;
-    float* sums = p.do_db ? reinterpret_cast<float*>(at + p.dz_bytes) : nullptr;
+    float* sums = p.do_db && !p.db_there ? reinterpret_cast<float*>(at + p.dz_bytes) : nullptr;
     float* partial = reinterpret_cast<float*>(at + p.dz_bytes + p.sums_bytes);
     if (p.store_dz || p.do_db) {
         p.z.dz = p.store_dz ? at : nullptr;
         p.z.sums = sums;
+        if (p.db_there) {
+            p.z.db = a->db.p;
+            p.z.db_member = a->db.member;
+        }
         e = launch_gradz(p.z, s);
         if (p.store_dz) p.dx.a = p.dw.a = at;
     }
-    if (e == hipSuccess && p.do_db) e = launch_bias_grad(a->dtype, sums, a->members, p.chunks, p.wide, a->db.p, a->db.member, s);
+    if (e == hipSuccess && p.do_db && !p.db_there) {
+        const bool sum = a->members != 1 && a->db.member == 0;
+        e = launch_bias_grad(a->dtype, sums, sum ? 1 : a->members, sum ? a->members * p.chunks : p.chunks, p.wide, a->db.p,
+                             a->db.member, s);
+    }
     if (e == hipSuccess && p.do_dx) e = launch_gemm(p.dx, partial, s);
     if (e == hipSuccess && p.do_dw) e = launch_gemm(p.dw, partial, s);
     return e == hipSuccess ? ES_OK : init_fail(ES_ERR_HIP, hipGetErrorString(e), who);

@@ -98,6 +98,20 @@ def test_large(dtype):
         _check(4, dtype, None, rows, k, f, "silu", gated=True)
 
 
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("members,rows,k,f", [
+    (200, 64, 8, 64), (200, 72, 136, 264), (2, 2568, 200, 2632),  # ragged tiles, one step, odd and even numbers of steps
+    (200, 264, 64, 72), (None, 4096, 128, 3088), (None, 3600, 192, 3856)])
+def test_many_tiles(dtype, members, rows, k, f):
+    """Products that fill the chip with tiles of the matrix cores' own kernels, whole 16-byte pieces; long ones' gradients
+    by sums over the members."""
+    _check(21, dtype, members, rows, k, f, "silu", residual=True)
+    _check(22, dtype, members, rows, k, f // 2, "gelu", gated=True, bias=False)
+    if members == 200:
+        _check(23, dtype, members, rows, k, f, "relu", shared_x=True)
+        _check(24, dtype, members, rows, k, f, "none", shared_w=True)
+
+
 def test_large_sums_over_members():
     """One network on many members, and one input for many networks: long reductions."""
     for dtype in TYPES:
