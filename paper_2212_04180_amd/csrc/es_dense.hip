@@ -220,7 +220,6 @@ __global__ __launch_bounds__(256) void k_gemm_join(GemmArgs a, int64_t total, ui
     const int64_t batch = total <= 0xFFFFFFFFll ? (uint32_t)row / (uint32_t)g.M : row / g.M;
     const int32_t o = inside ? (int32_t)((id - row * quads) * 4) : 0, left = g.N - o;
     const int64_t m = row - batch * g.M, wide = GATED ? 2 * (int64_t)g.N : g.N;
-    const bool vec = g.N % 4 == 0;
     float z[4] = {}, u[4] = {}, bz[4], bu[4], r[4];
     if (slice == 0) {
         load_bias<T, GATED, 4>(g, batch, o, bz, bu);
@@ -231,11 +230,11 @@ __global__ __launch_bounds__(256) void k_gemm_join(GemmArgs a, int64_t total, ui
 #pragma unroll 4
     for (int32_t s = slice; s < a.splits; s += slices, p += slices * pitch) {
         float v[4];
-        load_run<float, 4>(p, vec, left, v);
+        load_run<float, 4>(p, left, v);
 #pragma unroll
         for (int i = 0; i < 4; ++i) z[i] += v[i];
         if constexpr (GATED) {
-            load_run<float, 4>(p + g.N, vec, left, v);
+            load_run<float, 4>(p + g.N, left, v);
 #pragma unroll
             for (int i = 0; i < 4; ++i) u[i] += v[i];
         }
@@ -259,20 +258,11 @@ __global__ __launch_bounds__(256) void k_gemm_join(GemmArgs a, int64_t total, ui
     if (inside) finish<T, GATED, 4>(a, batch, m, o, z, u, bz, bu, r);
 }
 
-bool whole(const void* p, int64_t row, int64_t batch, int64_t rows, int64_t batches, size_t elem)
-{
-    return p && reinterpret_cast<uintptr_t>(p) % 16 == 0 && (rows <= 1 || row * elem % 16 == 0) &&
-           (batches <= 1 || batch * elem % 16 == 0);
-}
-
 GemmArgs plan(const Gemm& g)
 {
     GemmArgs a{};
     a.g = g;
     const size_t e = dtype_size(g.dtype);
-    a.vec_c = whole(g.c, g.c_row, g.c_batch, g.M, g.batches, dtype_size(g.c_dtype));
-    a.vec_res = whole(g.res, g.res_row, g.res_batch, g.M, g.batches, e);
-    a.vec_pre = whole(g.pre, g.pre_row, g.pre_batch, g.M, g.batches, e) && (!g.gated || g.N * e % 16 == 0);
     a.splits = 1;
     if (rows_fits(g)) {
         rows_plan(a);
@@ -345,7 +335,6 @@ struct GradZArgs {
     int64_t chunks;
     uint32_t colblocks;
     int32_t lx;
-    bool vec_dy, vec_pre;
 };
 
 template <typename T, bool GATED>
@@ -372,10 +361,10 @@ __global__ __launch_bounds__(256) void k_gradz(GradZArgs a)
         for (int r = ty; r < end; r += rows) {
             const int64_t row = row0 + r;
             float d[W], z[W], u[W], slope[W];
-            load_run<T, W>(dy + row * g.dy_row, a.vec_dy, left, d);
+            load_run<T, W>(dy + row * g.dy_row, left, d);
             if (GATED || g.act != ES_ACT_NONE) {
-                load_run<T, W>(pre + row * g.pre_row, a.vec_pre, left, z);
-                if constexpr (GATED) load_run<T, W>(pre + row * g.pre_row + g.out, a.vec_pre, left, u);
+                load_run<T, W>(pre + row * g.pre_row, left, z);
+                if constexpr (GATED) load_run<T, W>(pre + row * g.pre_row + g.out, left, u);
                 activate<FAST, true, W>(g.act, z, slope);
             }
 #pragma unroll
@@ -391,10 +380,9 @@ __global__ __launch_bounds__(256) void k_gradz(GradZArgs a)
                 }
             }
             if (g.dz) {
-                // rows of whole pieces; a gated layer's second half may start within one
                 T* dz = static_cast<T*>(g.dz) + (n * g.rows + row) * g.ldz + col;
-                store_run<T, W>(dz, true, left, GATED ? u : d);
-                if constexpr (GATED) store_run<T, W>(dz + g.out, g.out % W == 0, left, d);
+                store_run<T, W>(dz, left, GATED ? u : d);
+                if constexpr (GATED) store_run<T, W>(dz + g.out, left, d);
             }
         }
     }
@@ -488,8 +476,6 @@ hipError_t launch_gradz(const GradZ& g, hipStream_t s)
     const int64_t pieces = ((int64_t)g.out * e + 15) / 16;
     while (a.lx < 5 && (int64_t)1 << a.lx < pieces) ++a.lx;
     a.colblocks = (uint32_t)((pieces + (1 << a.lx) - 1) >> a.lx);
-    a.vec_dy = whole(g.dy, g.dy_row, g.dy_member, g.rows, g.members, e);
-    a.vec_pre = whole(g.pre, g.pre_row, g.pre_member, g.rows, g.members, e) && (!g.gated || g.out * e % 16 == 0);
     const int64_t grid = g.members * a.chunks * a.colblocks;
     if (grid == 0) return hipSuccess;
     auto go = [&](auto kernel) { kernel<<<(unsigned)grid, 256, 0, s>>>(a); };

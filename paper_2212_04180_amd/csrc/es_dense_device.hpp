@@ -131,37 +131,37 @@ struct GemmArgs {
     int32_t mt, nt, kt;    // tiles
     int32_t tile;          // staged: edge of a tile
     int64_t per;           // steps of a split
-    bool vec_c, vec_res, vec_pre;  // rows take 16-byte pieces
     float* partial;        // [splits][batches][M][N or 2 N]
 };
 
-// W consecutive elements of a row, `left` > 0 of them in it (the others repeat its last)
+// W consecutive elements of a row, `left` > 0 of them in it (the others repeat
+// its last).  16-byte accesses at any element's address: the target takes them.
 template <typename T, int W>
-__device__ __forceinline__ void load_run(const T* p, bool vec, int32_t left, float out[W])
+__device__ __forceinline__ void load_run(const T* p, int32_t left, float out[W])
 {
-    if (vec && left >= W) {
-        T t[W];
-        __builtin_memcpy(t, __builtin_assume_aligned(p, W * sizeof(T) < 16 ? W * sizeof(T) : 16), W * sizeof(T));
-#pragma unroll
-        for (int i = 0; i < W; ++i) out[i] = widen(t[i]);
+    T t[W];
+    if (left >= W) {
+        __builtin_memcpy(t, p, W * sizeof(T));
     } else {
 #pragma unroll
-        for (int i = 0; i < W; ++i) out[i] = widen(p[i < left ? i : left - 1]);  // no branches: all in flight at once
+        for (int i = 0; i < W; ++i) t[i] = p[i < left ? i : left - 1];  // no branches: all in flight at once
     }
+#pragma unroll
+    for (int i = 0; i < W; ++i) out[i] = widen(t[i]);
 }
 
 template <typename T, int W>
-__device__ __forceinline__ void store_run(T* p, bool vec, int32_t left, const float v[W])
+__device__ __forceinline__ void store_run(T* p, int32_t left, const float v[W])
 {
-    if (vec && left >= W) {
-        T t[W];
+    T t[W];
 #pragma unroll
-        for (int i = 0; i < W; ++i) t[i] = (T)v[i];
-        __builtin_memcpy(__builtin_assume_aligned(p, W * sizeof(T) < 16 ? W * sizeof(T) : 16), t, W * sizeof(T));
+    for (int i = 0; i < W; ++i) t[i] = (T)v[i];
+    if (left >= W) {
+        __builtin_memcpy(p, t, W * sizeof(T));
     } else {
 #pragma unroll
         for (int i = 0; i < W; ++i)
-            if (i < left) p[i] = (T)v[i];
+            if (i < left) p[i] = t[i];
     }
 }
 
@@ -171,7 +171,7 @@ __device__ __forceinline__ void load_res(const GemmArgs& a, int64_t batch, int64
 {
     const Gemm& g = a.g;
     if (g.res && n < g.N)
-        load_run<T, W>(static_cast<const T*>(g.res) + batch * g.res_batch + m * g.res_row + n, a.vec_res, g.N - n, r);
+        load_run<T, W>(static_cast<const T*>(g.res) + batch * g.res_batch + m * g.res_row + n, g.N - n, r);
     else
 #pragma unroll
         for (int i = 0; i < W; ++i) r[i] = 0.f;
@@ -194,8 +194,8 @@ __device__ __forceinline__ void finish(const GemmArgs& a, int64_t batch, int64_t
     }
     if (g.pre) {
         T* pre = static_cast<T*>(g.pre) + batch * g.pre_batch + m * g.pre_row + n;
-        store_run<T, W>(pre, a.vec_pre, left, z);
-        if constexpr (GATED) store_run<T, W>(pre + g.N, a.vec_pre, left, u);
+        store_run<T, W>(pre, left, z);
+        if constexpr (GATED) store_run<T, W>(pre + g.N, left, u);
     }
     activate<FAST, false, W>(g.act, z, nullptr);
     if constexpr (GATED) {
@@ -207,8 +207,8 @@ __device__ __forceinline__ void finish(const GemmArgs& a, int64_t batch, int64_t
         for (int i = 0; i < W; ++i) z[i] += r[i];
     }
     const int64_t at = batch * g.c_batch + m * g.c_row + n;
-    if (g.c_dtype == ES_F32) store_run<float, W>(static_cast<float*>(g.c) + at, a.vec_c, left, z);
-    else store_run<T, W>(static_cast<T*>(g.c) + at, a.vec_c, left, z);
+    if (g.c_dtype == ES_F32) store_run<float, W>(static_cast<float*>(g.c) + at, left, z);
+    else store_run<T, W>(static_cast<T*>(g.c) + at, left, z);
 }
 
 template <typename T, bool GATED, int W>
@@ -218,8 +218,8 @@ __device__ __forceinline__ void load_bias(const Gemm& g, int64_t batch, int32_t 
     for (int i = 0; i < W; ++i) bz[i] = bu[i] = 0.f;
     if (!g.bias || n >= g.N) return;
     const T* b = static_cast<const T*>(g.bias) + batch * g.bias_batch + n;
-    load_run<T, W>(b, false, g.N - n, bz);
-    if constexpr (GATED) load_run<T, W>(b + g.N, false, g.N - n, bu);
+    load_run<T, W>(b, g.N - n, bz);
+    if constexpr (GATED) load_run<T, W>(b + g.N, g.N - n, bu);
 }
 
 // Partial sums of W consecutive outputs
@@ -231,9 +231,8 @@ __device__ __forceinline__ void store_partial(const GemmArgs& a, int32_t split, 
     const int32_t left = g.N - n;
     if (left <= 0) return;
     float* p = a.partial + ((split * g.batches + batch) * g.M + m) * (GATED ? 2 * (int64_t)g.N : g.N) + n;
-    const bool vec = g.N % 4 == 0;
-    store_run<float, W>(p, vec, left, z);
-    if constexpr (GATED) store_run<float, W>(p + g.N, vec, left, u);
+    store_run<float, W>(p, left, z);
+    if constexpr (GATED) store_run<float, W>(p + g.N, left, u);
 }
 
 // Bytes of LDS that a wave's epilogue takes: 32 rows of its NB column tiles.
