@@ -258,21 +258,115 @@ __global__ __launch_bounds__(256) void k_gemm_join(GemmArgs a, int64_t total, ui
     if (inside) finish<T, GATED, 4>(a, batch, m, o, z, u, bz, bu, r);
 }
 
-GemmArgs plan(const Gemm& g)
+// ---- copies in whole pieces ------------------------------------------------
+// One operand as [n][rows][ld], ld a multiple of 8 elements, zeros behind its
+// columns.  Bound by memory.  Rows of 16-bit elements at odd multiples of 2 bytes
+// are read in aligned words and shifted: 16-byte loads at such addresses run at
+// less than half the rate (rows of 4095 bf16 1.9 TB/s, of 4098 4.5).
+struct PackArgs {
+    const uint16_t* src;
+    uint16_t* dst;
+    int64_t n, rows, cols, ld, batch, row, total;  // total: pieces
+};
+
+__global__ __launch_bounds__(256) void k_pack(PackArgs a)
 {
-    GemmArgs a{};
-    a.g = g;
-    const size_t e = dtype_size(g.dtype);
-    a.splits = 1;
-    if (rows_fits(g)) {
-        rows_plan(a);
-        return a;
+    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x, per = a.ld / 8;
+    if (id >= a.total) return;
+    const int64_t r = a.total <= 0xFFFFFFFFll ? (uint32_t)id / (uint32_t)per : id / per;  // n * rows + row
+    const int64_t n = a.total <= 0xFFFFFFFFll ? (uint32_t)r / (uint32_t)a.rows : r / a.rows;
+    const int64_t c = (id - r * per) * 8, left = a.cols - c;
+    const uint16_t* p = a.src + n * a.batch + (r - n * a.rows) * a.row + c;
+    uintx4 v;
+    if (left >= 8) {
+        const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+        const uint32_t* w = reinterpret_cast<const uint32_t*>(at & ~(uintptr_t)3);  // words that hold the 8 elements
+        const uint32_t sh = (uint32_t)(at & 2) * 8;
+        uint32_t t[4];
+        __builtin_memcpy(t, w, 16);
+        const uint32_t last = w[sh ? 4 : 3];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = __builtin_amdgcn_alignbit(i < 3 ? t[i + 1] : last, t[i], sh);
+    } else {
+        uint16_t t[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) t[i] = i < left ? p[i] : (uint16_t)0;
+        __builtin_memcpy(&v, t, 16);
     }
-    if (large_fits(g)) {
-        large_plan(a);
-        return a;
-    }
-    const int32_t kt = 128 / (int32_t)e;
+    *reinterpret_cast<uintx4*>(a.dst + id * 8) = v;
+}
+
+struct Packing {
+    bool a, b;
+    size_t a_bytes, b_bytes;
+};
+
+int64_t pack_rows(const Gemm& g, bool is_a) { return (is_a ? g.a_kmajor : g.b_kmajor) ? (is_a ? g.M : (g.gated ? 2 : 1) * (int64_t)g.N) : g.K; }
+int64_t pack_cols(const Gemm& g, bool is_a) { return (is_a ? g.a_kmajor : g.b_kmajor) ? g.K : is_a ? g.M : g.N; }
+
+// The product on copies: sets the operand's place (base: where the copy will be)
+// and the bytes that it takes.
+size_t pack_operand(Gemm& g, bool is_a, void* base)
+{
+    const int64_t rows = pack_rows(g, is_a), ld = (pack_cols(g, is_a) + 7) / 8 * 8;
+    // an operand that all batches (or all terms of the reduction) share is copied once
+    const int64_t batch = is_a ? g.a_batch : g.b_batch, red = is_a ? g.a_red : g.b_red;
+    const int64_t n = g.batches > 1 ? (batch ? g.batches : 1) : g.red > 1 && red ? g.red : 1;
+    (is_a ? g.a : g.b) = base;
+    (is_a ? g.a_row : g.b_row) = ld;
+    (is_a ? g.a_batch : g.b_batch) = g.batches > 1 && batch ? rows * ld : 0;
+    (is_a ? g.a_red : g.b_red) = g.batches <= 1 && g.red > 1 && red ? rows * ld : 0;
+    (is_a ? g.a_padded : g.b_padded) = true;
+    return workspace_up((size_t)n * rows * ld * 2);
+}
+
+// Whether operands are copied for the large tiles: those that they do not take as
+// they lie (both where the k of a row ends within a piece), if the staged kernel's
+// further time (about 450 TFLOP/s against 1100, measured at 8192 x 4095 x 4095:
+// forward 404 us against 218 and the copies' 50) is more than the copies'.
+Packing packing(const Gemm& g)
+{
+    Packing p{};
+    if (g.dtype == ES_F32 || g.K == 0 || g.red == 0 || g.batches == 0) return p;
+    const bool whole_k = g.K % 8 == 0;
+    p.a = !large_takes(g, true) || (g.a_kmajor && !whole_k && !g.a_padded);
+    p.b = !large_takes(g, false) || (g.b_kmajor && !whole_k && !g.b_padded);
+    if (!p.a && !p.b) return p;
+    Gemm h = g;
+    // any aligned address serves for the look
+    if (p.a) p.a_bytes = pack_operand(h, true, reinterpret_cast<void*>(WORKSPACE_ALIGN));
+    if (p.b) p.b_bytes = pack_operand(h, false, reinterpret_cast<void*>(WORKSPACE_ALIGN));
+    const double flops = 2.0 * g.batches * g.red * g.M * (g.gated ? 2.0 : 1.0) * g.N * g.K;
+    const double gain = flops * (1 / 450e12 - 1 / 1100e12), cost = 2.0 * (p.a_bytes + p.b_bytes) / 4e12 + 4e-6 * (p.a + p.b);
+    if (gain <= cost || !large_fits(h)) return Packing{};
+    return p;
+}
+
+hipError_t launch_pack(const Gemm& from, const Gemm& to, bool is_a, hipStream_t s)
+{
+    PackArgs a{};
+    a.src = static_cast<const uint16_t*>(is_a ? from.a : from.b);
+    a.dst = static_cast<uint16_t*>(const_cast<void*>(is_a ? to.a : to.b));
+    a.rows = pack_rows(from, is_a);
+    a.cols = pack_cols(from, is_a);
+    a.ld = is_a ? to.a_row : to.b_row;
+    const int64_t batch = is_a ? from.a_batch : from.b_batch, red = is_a ? from.a_red : from.b_red;
+    a.n = from.batches > 1 ? (batch ? from.batches : 1) : from.red > 1 && red ? from.red : 1;
+    a.batch = from.batches > 1 ? batch : red;
+    a.row = is_a ? from.a_row : from.b_row;
+    a.total = a.n * a.rows * (a.ld / 8);
+    if ((a.total + 255) / 256 > 0x7FFFFFFF) return hipErrorInvalidValue;  // beyond any memory
+    k_pack<<<(unsigned)((a.total + 255) / 256), 256, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+// Kernel, tiles and splits of a.g
+void plan_path(GemmArgs& a)
+{
+    const Gemm& g = a.g;
+    if (rows_fits(g)) return rows_plan(a);
+    if (large_fits(g)) return large_plan(a);
+    const int32_t kt = 128 / (int32_t)dtype_size(g.dtype);
     a.path = PATH_STAGED;
     a.kt = g.K ? (g.K - 1) / kt + 1 : 0;
     a.tile = 128;
@@ -288,6 +382,23 @@ GemmArgs plan(const Gemm& g)
     if (tiles < 512 && steps >= 8) splits = std::min((1024 + tiles - 1) / tiles, steps / 4);
     a.per = steps ? (steps + splits - 1) / splits : 0;
     a.splits = steps ? (int32_t)((steps + a.per - 1) / a.per) : 1;
+}
+
+GemmArgs plan(const Gemm& from, void* workspace, size_t* bytes)
+{
+    GemmArgs a{};
+    Gemm g = from;
+    const Packing pk = packing(g);
+    char* at = static_cast<char*>(workspace);
+    if (pk.a) pack_operand(g, true, at);
+    if (pk.b) pack_operand(g, false, at + pk.a_bytes);
+    a.g = g;
+    a.partial = reinterpret_cast<float*>(at + pk.a_bytes + pk.b_bytes);
+    a.splits = 1;
+    plan_path(a);
+    *bytes = pk.a_bytes + pk.b_bytes;
+    if (a.path != PATH_ROWS && a.splits > 1)
+        *bytes += workspace_up((size_t)4 * a.splits * g.batches * g.M * (g.gated ? 2 : 1) * (size_t)g.N);
     return a;
 }
 
@@ -381,8 +492,18 @@ __global__ __launch_bounds__(256) void k_gradz(GradZArgs a)
             }
             if (g.dz) {
                 T* dz = static_cast<T*>(g.dz) + (n * g.rows + row) * g.ldz + col;
-                store_run<T, W>(dz, left, GATED ? u : d);
-                if constexpr (GATED) store_run<T, W>(dz + g.out, left, d);
+                // zeros up to the end of the row's last piece
+                if constexpr (GATED) {
+                    store_run<T, W>(dz, left, u);
+                    store_run<T, W>(dz + g.out, left, d);
+                    if (left <= W)
+                        for (int64_t i = 2 * (int64_t)g.out; i < g.ldz; ++i) dz[i - col] = (T)0.f;
+                } else {
+#pragma unroll
+                    for (int i = 0; i < W; ++i)
+                        if (i >= left) d[i] = 0.f;
+                    store_run<T, W>(dz, W, d);
+                }
             }
         }
     }
@@ -431,25 +552,31 @@ __global__ __launch_bounds__(1024) void k_bias_grad(const float* sums, int64_t c
 
 }  // namespace
 
-size_t gemm_workspace_floats(const Gemm& g)
+size_t gemm_workspace(const Gemm& g)
 {
-    const GemmArgs a = plan(g);
-    return a.path != PATH_ROWS && a.splits > 1 ? (size_t)a.splits * g.batches * g.M * (g.gated ? 2 : 1) * (size_t)g.N : 0;
+    size_t n = 0;
+    plan(g, reinterpret_cast<void*>(WORKSPACE_ALIGN), &n);
+    return n;
 }
 
 bool gemm_too_large(const Gemm& g)
 {
-    const GemmArgs a = plan(g);
+    size_t n = 0;
+    const GemmArgs a = plan(g, reinterpret_cast<void*>(WORKSPACE_ALIGN), &n);
     const __int128 most = 0x7FFFFFFF;
     if (a.path == PATH_ROWS) return (__int128)g.batches * a.nt > most;
     return (__int128)g.batches * a.splits * a.mt * a.nt > most ||
            (a.splits > 1 && (__int128)g.batches * g.M * join_quads(g) / 256 >= most);
 }
 
-hipError_t launch_gemm(const Gemm& g, float* partial, hipStream_t s)
+hipError_t launch_gemm(const Gemm& g, void* workspace, hipStream_t s)
 {
-    GemmArgs a = plan(g);
-    a.partial = partial;
+    size_t n = 0;
+    const GemmArgs a = plan(g, workspace, &n);
+    hipError_t e = hipSuccess;
+    if (a.g.a != g.a) e = launch_pack(g, a.g, true, s);
+    if (e == hipSuccess && a.g.b != g.b) e = launch_pack(g, a.g, false, s);
+    if (e != hipSuccess) return e;
     switch (g.dtype) {
     case ES_BF16: return launch_typed<__bf16>(a, s);
     case ES_F16: return launch_typed<_Float16>(a, s);

@@ -9,6 +9,8 @@
 
 namespace esmi {
 
+constexpr size_t WORKSPACE_ALIGN = 256;
+constexpr size_t workspace_up(size_t n) { return (n + WORKSPACE_ALIGN - 1) / WORKSPACE_ALIGN * WORKSPACE_ALIGN; }
 constexpr size_t dtype_size(int32_t t) { return t == ES_F32 ? 4 : 2; }
 
 // One matrix product per batch, C[m][n] = sum over r < red and k < K of
@@ -23,6 +25,9 @@ struct Gemm {
     int64_t a_batch, a_red, a_row;  // element strides; a_row between rows of the memory's matrix
     int64_t b_batch, b_red, b_row;
     bool a_kmajor, b_kmajor;
+    // rows begin at multiples of 16 bytes and zeros follow them up to the next
+    // one, readable memory in any case (16-bit types)
+    bool a_padded, b_padded;
     // gated: N counts the outputs; B has 2 N rows, the gates' first
     bool gated;
     int32_t act;
@@ -37,10 +42,10 @@ struct Gemm {
     int32_t c_dtype;
 };
 
-// Floats of partial sums that the product keeps between its two launches
-// where its reduction is split (0: one launch).
-size_t gemm_workspace_floats(const Gemm& g);
-hipError_t launch_gemm(const Gemm& g, float* partial, hipStream_t s);
+// Bytes that the product keeps between its launches: copies of operands in whole
+// pieces, partial sums where its reduction is split (0: one launch).
+size_t gemm_workspace(const Gemm& g);
+hipError_t launch_gemm(const Gemm& g, void* workspace, hipStream_t s);
 bool gemm_too_large(const Gemm& g);  // more workgroups than a launch holds
 
 // dz = dy act'(pre) (or both halves of a gated layer) in the type, rows of

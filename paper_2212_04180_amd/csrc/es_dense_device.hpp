@@ -125,7 +125,7 @@ __device__ __forceinline__ floatx4 product(uintx4 a, uintx4 b, floatx4 c)
 enum GemmPath { PATH_STAGED, PATH_LARGE, PATH_ROWS };
 
 struct GemmArgs {
-    Gemm g;
+    Gemm g;  // on the packed copies, if any
     int32_t path;
     int32_t splits;        // of the reduction; 1: C is finished here (few rows: among a workgroup's waves)
     int32_t mt, nt, kt;    // tiles
@@ -295,6 +295,7 @@ __device__ __forceinline__ void epilogue(const GemmArgs& a, int32_t split, int64
 bool rows_fits(const Gemm& g);
 void rows_plan(GemmArgs& a);
 hipError_t launch_rows(const GemmArgs& a, hipStream_t s);
+bool large_takes(const Gemm& g, bool is_a);
 bool large_fits(const Gemm& g);
 void large_plan(GemmArgs& a);
 hipError_t launch_large(const GemmArgs& a, hipStream_t s);

@@ -407,15 +407,21 @@ bool pieces(const Gemm& g, const void* p, int64_t row, int64_t batch, int64_t re
 
 }  // namespace
 
-// 16-bit operands in whole 16-byte pieces (addresses, strides, and the sizes
-// along which they are contiguous), offsets within a tile's reach that fit the
-// buffer loads' 31 bits, and enough tiles or steps to be worth it.
+// Whether an operand can be fetched in whole 16-byte pieces as it lies: its
+// addresses, strides, and the size along which it is contiguous.
+bool large_takes(const Gemm& g, bool is_a)
+{
+    const bool kmajor = is_a ? g.a_kmajor : g.b_kmajor, padded = is_a ? g.a_padded : g.b_padded;
+    return (is_a ? pieces(g, g.a, g.a_row, g.a_batch, g.a_red) : pieces(g, g.b, g.b_row, g.b_batch, g.b_red)) &&
+           (padded || (kmajor ? g.K : is_a ? g.M : g.N) % 8 == 0);
+}
+
+// 16-bit operands in whole pieces, offsets within a tile's reach that fit the
+// buffer loads' 31 bits, and at least a quarter of a tile.
 bool large_fits(const Gemm& g)
 {
     if (g.dtype == ES_F32 || g.K == 0 || g.red == 0 || g.red * ((g.K - 1) / BK + 1) > 0x7FFFFFFF) return false;
-    if (!pieces(g, g.a, g.a_row, g.a_batch, g.a_red) || !pieces(g, g.b, g.b_row, g.b_batch, g.b_red)) return false;
-    if ((g.a_kmajor || g.b_kmajor) && g.K % 8) return false;
-    if ((!g.a_kmajor && g.M % 8) || (!g.b_kmajor && g.N % 8)) return false;
+    if (!large_takes(g, true) || !large_takes(g, false)) return false;
     // the buffers' ranges end k rows: these lie behind each other
     if ((!g.a_kmajor && g.a_row < g.M) || (!g.b_kmajor && g.b_row < g.N)) return false;
     const int64_t reach = (int64_t)1 << 30;

@@ -15,9 +15,9 @@ using namespace esmi;
 namespace {
 
 constexpr int64_t kMaxDim = 0x7FFFFFFF;
-constexpr size_t kAlign = 256;
+constexpr size_t kAlign = WORKSPACE_ALIGN;
 
-size_t up(size_t n) { return (n + kAlign - 1) / kAlign * kAlign; }
+size_t up(size_t n) { return workspace_up(n); }
 
 bool dtype_ok(int32_t t) { return t == ES_F32 || t == ES_BF16 || t == ES_F16; }
 
@@ -118,7 +118,7 @@ es_status forward(const es_dense_args* a, bool gated, const char* who, void* ws,
     const Gemm g = forward_gemm(*a, gated);
     const bool empty = g.batches == 0 || g.M == 0 || g.N == 0;
     if (!empty && gemm_too_large(g)) return init_fail(ES_ERR_UNSUPPORTED, "more workgroups than a launch holds", who);
-    const size_t want = empty ? 0 : up(4 * gemm_workspace_floats(g));
+    const size_t want = empty ? 0 : gemm_workspace(g);
     if (need) {
         *need = want;
         return ES_OK;
@@ -126,7 +126,7 @@ es_status forward(const es_dense_args* a, bool gated, const char* who, void* ws,
     if (bytes < want) return init_fail(ES_ERR_ARG, "the workspace is too small", who);
     if (want && reinterpret_cast<uintptr_t>(ws) % kAlign) return init_fail(ES_ERR_ARG, "the workspace is not aligned", who);
     if (empty) return ES_OK;
-    const hipError_t e = launch_gemm(g, static_cast<float*>(ws), static_cast<hipStream_t>(stream));
+    const hipError_t e = launch_gemm(g, ws, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? ES_OK : init_fail(ES_ERR_HIP, hipGetErrorString(e), who);
 }
 
@@ -188,7 +188,7 @@ BackwardPlan plan_backward(const es_dense_grad_args& a, bool gated)
     // dx[i][k] = sum_o dz[i][o] w[o][k]
     p.dx = g;
     p.dx.M = (int32_t)B; p.dx.N = (int32_t)a.in; p.dx.K = (int32_t)wide;
-    p.dx.a = a.dy.p; p.dx.a_row = z_row; p.dx.a_kmajor = true;
+    p.dx.a = a.dy.p; p.dx.a_row = z_row; p.dx.a_kmajor = true; p.dx.a_padded = p.store_dz;
     p.dx.b = a.w.p; p.dx.b_row = a.w.row; p.dx.b_kmajor = false;
     p.dx.c = a.dx.p; p.dx.c_row = a.dx.row; p.dx.c_batch = a.dx.member;
     if (sum_dx) {
@@ -203,7 +203,7 @@ BackwardPlan plan_backward(const es_dense_grad_args& a, bool gated)
     // dw[o][k] = sum_i dz[i][o] x[i][k]
     p.dw = g;
     p.dw.M = (int32_t)wide; p.dw.N = (int32_t)a.in; p.dw.K = (int32_t)B;
-    p.dw.a = a.dy.p; p.dw.a_row = z_row; p.dw.a_kmajor = false;
+    p.dw.a = a.dy.p; p.dw.a_row = z_row; p.dw.a_kmajor = false; p.dw.a_padded = p.store_dz;
     p.dw.b = a.x.p; p.dw.b_row = a.x.row; p.dw.b_kmajor = false;
     p.dw.c = a.dw.p; p.dw.c_row = a.dw.row; p.dw.c_batch = a.dw.member;
     if (sum_dw) {
@@ -216,9 +216,9 @@ BackwardPlan plan_backward(const es_dense_grad_args& a, bool gated)
         p.dw.batches = n; p.dw.red = 1; p.dw.a_batch = z_member; p.dw.b_batch = a.x.member;
     }
     size_t f = 0;
-    if (p.do_dx) f = std::max(f, gemm_workspace_floats(p.dx));
-    if (p.do_dw) f = std::max(f, gemm_workspace_floats(p.dw));
-    p.partial_bytes = up(4 * f);
+    if (p.do_dx) f = std::max(f, gemm_workspace(p.dx));
+    if (p.do_dw) f = std::max(f, gemm_workspace(p.dw));
+    p.partial_bytes = f;
     return p;
 }
 
@@ -243,7 +243,7 @@ es_status backward(const es_dense_grad_args* a, bool gated, const char* who, voi
     hipStream_t s = static_cast<hipStream_t>(stream);
     hipError_t e = hipSuccess;
     float* sums = p.do_db && !p.db_there ? reinterpret_cast<float*>(at + p.dz_bytes) : nullptr;
-    float* partial = reinterpret_cast<float*>(at + p.dz_bytes + p.sums_bytes);
+    void* partial = at + p.dz_bytes + p.sums_bytes;
     if (p.store_dz || p.do_db) {
         p.z.dz = p.store_dz ? at : nullptr;
         p.z.sums = sums;

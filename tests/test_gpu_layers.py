@@ -112,6 +112,26 @@ def test_many_tiles(dtype, members, rows, k, f):
         _check(24, dtype, members, rows, k, f, "none", shared_w=True)
 
 
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("members,rows,k,f,kw", [
+    (None, 4100, 1031, 2051, {}), (None, 2049, 2052, 2047, {}), (3, 2050, 1031, 1029, {}), (3, 1401, 1031, 2051, dict(shared_w=True)),
+    (3, 1401, 1031, 2051, dict(shared_x=True))])
+def test_large_and_ragged(dtype, members, rows, k, f, kw):
+    """Sizes whose operands are copied into whole 16-byte pieces first, odd addresses among them."""
+    _check(25, dtype, members, rows, k, f, "tanh", **kw)
+    _check(26, dtype, members, rows, k, f // 2, "silu", gated=True, bias=False, **kw)
+
+
+def test_large_and_ragged_without_activation():
+    """dy itself is the operand: odd rows, a padded view with NaN in its gaps."""
+    P = _P()
+    x, w, b, _, dy = _case(27, BF, None, 2049, 2050, 2051, "none")
+    big = torch.full((2049, 2060), float("nan"), dtype=BF, device="cuda")
+    big[:, 3:2054] = dy
+    for name, got, (v, bound) in zip(("dx", "dw", "db"), P.dense_backward(big[:, 3:2054], x, w), L.backward(dy, x, w, None)):
+        L.check(name, got, v, bound)
+
+
 def test_large_sums_over_members():
     """One network on many members, and one input for many networks: long reductions."""
     for dtype in TYPES:
