@@ -1,22 +1,18 @@
 // es_dense_large.hip -- the matrix products of 16-bit layers at sizes where the
 // matrix cores bound them, gfx950.
 //
-// A workgroup of four waves makes a 256 x 128 tile of C, each wave 128 x 64 of
-// it (8 x 4 tiles of v_mfma_f32_16x16x32, 128 accumulators a lane).  Steps of 32
-// along k pass through three LDS buffers of 24 KB, filled by loads that go from
-// memory to LDS without registers and are two steps ahead; one barrier a step.
-// Two workgroups fit a CU (144 KB of LDS, 8 waves): where one waits at its
-// barrier, starts up or is in its epilogue, the other's products go on.  A
-// wave reads 12 fragments of 1 KB from LDS for 32 products of 16 cycles.
+// k_gemm_wide   256 x 256 tiles of C, for products that fill the chip with them
+// k_gemm_mid    128 x 128 tiles
+// Steps along k pass through buffers in LDS, filled by loads that go there from
+// memory without registers, ahead of their use.
 //
 // The loads write LDS in lane order, so the spreading over its banks is done by
 // which 16 bytes a lane fetches:
-//   k-major operand (k contiguous): 64 bytes of k a row; piece c of row r lies at
+//   k-major operand (k contiguous): 128 bytes of k a row; piece c of row r lies at
 //     position c ^ f(r).  A 16-byte read serves lanes {0-3, 12-15, 20-27},
 //     {4-11, 16-19, 28-31} and those + 32 together (measured), so the rows 4-11 of
-//     a fragment meet the other rows' next piece: f is 3 for its upper 8 rows,
-//     which spreads each such 16 over all banks (any f that spreads 16 lanes in
-//     a row costs twice the cycles);
+//     a fragment meet the other rows' next piece: f spreads each such 16 over all
+//     banks (one that spreads 16 lanes in a row costs twice the cycles);
 //   else: a row of m (n) per k, read back transposed by ds_read_b64_tr_b16, which
 //     hands lane i of 16 the four k of column i.
 // Rows, columns and k beyond the matrices are not fetched: a buffer load out of
@@ -30,8 +26,6 @@ namespace esmi {
 
 namespace {
 
-constexpr int BM = 256, BN = 128, BK = 32, STAGES = 3;  // k_gemm_large
-constexpr int A_BYTES = BM * BK * 2, B_BYTES = BN * BK * 2, STAGE_BYTES = A_BYTES + B_BYTES;
 constexpr uint32_t OUT = 0x80000000u;  // an offset beyond every buffer's range
 
 typedef __attribute__((address_space(3))) void lds_void;
@@ -49,7 +43,6 @@ struct Operand {
     static __device__ __forceinline__ int f(int r)
     {
         const int a = (r >> 2) & 3;
-        if constexpr (STEP == 32) return 3 * (a >> 1);
         return (2 * a + ((r >> 1) & 1)) ^ ((a ^ (a >> 1)) & 1);
     }
     // pairs of pieces (16 columns) of different k rows on different banks
@@ -127,30 +120,37 @@ __device__ __forceinline__ void tile_of(uint32_t id, uint32_t mt, uint32_t nt, i
     tn = __builtin_amdgcn_readfirstlane(in / rows);
 }
 
-template <typename T, bool AK, bool BKM, bool GATED>
-__global__ __launch_bounds__(256, 2) void k_gemm_large(GemmArgs a)
+// 128 x 128 tiles.  Four waves, 64 x 64 each; steps of 64 k through a ring of
+// STAGES buffers of 32 KB, one barrier a step: the loads are STAGES - 1 steps
+// ahead.  With two stages two workgroups share a CU and cover each other's
+// barriers and epilogues; a launch of at most one a CU has four stages instead,
+// and issues its loads between the products.  2048^3 bf16 29 us, 590 TFLOP/s.
+constexpr int MT = 128, MK = 64, M_BYTES = MT * MK * 2;  // of one operand's buffer
+
+template <typename T, bool AK, bool BKM, bool GATED, int STAGES>
+__global__ __launch_bounds__(256, 2) void k_gemm_mid(GemmArgs a)
 {
     extern __shared__ __align__(1024) unsigned char lds[];
     const Gemm& g = a.g;
-    constexpr int OUTS = GATED ? BN / 2 : BN;  // outputs of a tile
+    constexpr int OUTS = GATED ? MT / 2 : MT;  // outputs of a tile
     const uint32_t tiles = (uint32_t)a.mt * a.nt, outer = blockIdx.x / tiles;
     int32_t tm, tn;
     tile_of(blockIdx.x % tiles, a.mt, a.nt, tm, tn);
     const int32_t split = __builtin_amdgcn_readfirstlane(outer % a.splits);
     const int64_t batch = (uint32_t)__builtin_amdgcn_readfirstlane(outer / a.splits);
-    const int32_t m0 = tm * BM, n0 = tn * OUTS;
+    const int32_t m0 = tm * MT, n0 = tn * OUTS;
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int wm = wave / 2, wn = wave % 2;
     const int32_t steps = (int32_t)g.red * a.kt;  // below 2^31
-    const int32_t per = (int32_t)a.per, first = split * per, last = steps - first < per ? steps : first + per;
+    const int32_t per = (int32_t)a.per, first = split * per, count = steps - first < per ? steps - first : per;
 
-    // bases at the tile's first row (k-major) or column
-    const T* A = static_cast<const T*>(g.a) + batch * g.a_batch + (AK ? m0 * g.a_row : 0);
-    const T* B = static_cast<const T*>(g.b) + batch * g.b_batch + (BKM && !GATED ? n0 * g.b_row : 0);
-    using OA = Operand<AK, BM, BK, 256>;
-    using OB = Operand<BKM, BN, BK, 256>;
+    using OA = Operand<AK, MT, MK, 256>;
+    using OB = Operand<BKM, MT, MK, 256>;
     OA oa;
     OB ob;
+    // bases at the tile's first row (k-major) or column
+    const T* pa = static_cast<const T*>(g.a) + batch * g.a_batch + (AK ? m0 * g.a_row : 0);
+    const T* pb = static_cast<const T*>(g.b) + batch * g.b_batch + (BKM && !GATED ? n0 * g.b_row : 0);
     oa.init(g.a_row, [&](int i) -> int64_t { return m0 + i < g.M ? (AK ? i : m0 + i) : -1; });
     if constexpr (GATED) {
         // 32 gates, then their 32 others, for each wave's 64
@@ -161,67 +161,84 @@ __global__ __launch_bounds__(256, 2) void k_gemm_large(GemmArgs a)
     } else {
         ob.init(g.b_row, [&](int i) -> int64_t { return n0 + i < g.N ? (BKM ? i : n0 + i) : -1; });
     }
-
-    floatx4 acc[8][4];  // [m tile][n tile]
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
-
-    // the next step to fetch, and the buffers of the next fetch and of this step
-    int32_t kt = first, to = 0, from = 0;
-    const T *pa = A, *pb = B;
+    // the next step to fetch
+    int32_t kt = first;
     if (a.splits > 1 && g.red > 1) {
         const int32_t r = __builtin_amdgcn_readfirstlane((uint32_t)first / (uint32_t)a.kt);
         kt = first - r * a.kt;
         pa += r * g.a_red;
         pb += r * g.b_red;
     }
-    auto fetch = [&](int32_t t) {
-        if (t >= last) return;
-        const int32_t k0 = kt * BK;
-        oa.fetch(pa + (AK ? (int64_t)k0 : k0 * g.a_row), g.a_row, g.K - k0, lds + to);
-        ob.fetch(pb + (BKM ? (int64_t)k0 : k0 * g.b_row), g.b_row, g.K - k0, lds + to + A_BYTES);
-        to = to == (STAGES - 1) * STAGE_BYTES ? 0 : to + STAGE_BYTES;
+    auto fetch = [&](int32_t t) {  // step t of this workgroup's; behind the last one nothing is fetched
+        const int32_t k0 = kt * MK, left = t < count ? g.K - k0 : 0;
+        unsigned char* to = lds + (t % STAGES) * 2 * M_BYTES;
+        oa.fetch(pa + (AK ? (int64_t)k0 : k0 * g.a_row), g.a_row, left, to);
+        ob.fetch(pb + (BKM ? (int64_t)k0 : k0 * g.b_row), g.b_row, left, to + M_BYTES);
         if (++kt == a.kt) {
             kt = 0;
             pa += g.a_red;
             pb += g.b_red;
         }
     };
-    static_assert(OA::LOADS + OB::LOADS == 6, "loads per step, counted below");
-    fetch(first);
-    fetch(first + 1);
-    for (int32_t t = first; t < last; ++t) {
-        // this step's loads are done once only the next step's are in flight
-        if (t + 1 < last) asm volatile("s_waitcnt vmcnt(6) lgkmcnt(0)" ::: "memory");
+
+    floatx4 acc[4][4];  // [m tile][n tile]
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+    static_assert(OA::LOADS + OB::LOADS == 8 && (STAGES == 2 || STAGES == 4), "loads per step, counted below");
+    for (int s = 0; s + 1 < STAGES; ++s) fetch(s);
+    for (int32_t t = 0; t < count; ++t) {
+        // this step's loads are done once only the later steps' are in flight
+        if constexpr (STAGES == 4) asm volatile("s_waitcnt vmcnt(16) lgkmcnt(0)" ::: "memory");
         else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        // every wave has left the buffer that this fills
-        fetch(t + 2);
-        const unsigned char* now = lds + from;
-        from = from == (STAGES - 1) * STAGE_BYTES ? 0 : from + STAGE_BYTES;
-        uintx4 fb[4];
+        // the step to fetch: every wave has left the buffer that it fills
+        const int32_t k0 = kt * MK, left = t + STAGES - 1 < count ? g.K - k0 : 0;
+        unsigned char* to = lds + ((t + STAGES - 1) % STAGES) * 2 * M_BYTES;
+        const T* ba = pa + (AK ? (int64_t)k0 : k0 * g.a_row);
+        const T* bb = pb + (BKM ? (int64_t)k0 : k0 * g.b_row);
+        if (++kt == a.kt) {
+            kt = 0;
+            pa += g.a_red;
+            pb += g.b_red;
+        }
+        if constexpr (STAGES == 2) {
+            oa.fetch(ba, g.a_row, left, to);
+            ob.fetch(bb, g.b_row, left, to + M_BYTES);
+        }
+        const unsigned char* now = lds + (t % STAGES) * 2 * M_BYTES;
+        uintx4 fa[2][4], fb[2][4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) fb[j] = OB::read(now + A_BYTES, 64 * wn, j, 0, lane);
-        uintx4 fa[8];
+        for (int ks = 0; ks < 2; ++ks) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) fa[i] = OA::read(now, 128 * wm, i, 0, lane);
+            for (int j = 0; j < 4; ++j) fb[ks][j] = OB::read(now + M_BYTES, 64 * wn, j, ks, lane);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) fa[ks][i] = OA::read(now, 64 * wm, i, ks, lane);
+        }
         // all reads under way before the first product: left to itself the compiler
         // reads two fragments at a time and waits for each
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+        for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) acc[i][j] = product<T>(fb[j], fa[i], acc[i][j]);
+            for (int i = 0; i < 4; ++i) {
+                if constexpr (STAGES == 4) {
+                    if (ks == 0) oa.load(i, ba, g.a_row, left, to);
+                    else ob.load(i, bb, g.b_row, left, to + M_BYTES);
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) acc[i][j] = product<T>(fb[ks][j], fa[ks][i], acc[i][j]);
+                if constexpr (STAGES == 4) __builtin_amdgcn_sched_barrier(0);
+            }
     }
-
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     __syncthreads();  // the buffers serve the epilogue
-    epilogue<T, GATED, 8, 4>(a, split, batch, m0 + 128 * wm, n0 + (GATED ? 32 : 64) * wn, acc,
+    epilogue<T, GATED, 4, 4>(a, split, batch, m0 + 64 * wm, n0 + (GATED ? 32 : 64) * wn, acc,
                              reinterpret_cast<float*>(lds + wave * EPILOGUE_LDS<4>), lane);
 }
-static_assert(4 * EPILOGUE_LDS<4> <= STAGES * STAGE_BYTES, "the epilogue's rows fit the buffers");
+static_assert(4 * EPILOGUE_LDS<4> <= 2 * 2 * M_BYTES, "the epilogue's rows fit the buffers");
 
 // 256 x 256 tiles for products that fill the chip with them.  Eight waves, 128 x
 // 64 each, in two groups of one wave a SIMD, half a step of 32 k apart: while
@@ -378,25 +395,28 @@ __global__ __launch_bounds__(512, 2) void k_gemm_wide(GemmArgs a)
 }
 static_assert(8 * EPILOGUE_LDS<4> <= 4 * W_BYTES, "the epilogue's rows fit the buffers");
 
+template <typename T, bool AK, bool BKM, bool GATED>
+hipError_t launch_kernel(const GemmArgs& a, hipStream_t s)
+{
+    const unsigned grid = (unsigned)(a.g.batches * a.splits * a.mt * a.nt);
+    const bool wide = a.tile == WT, deep = grid <= 256;
+    void (*kernel)(GemmArgs) = wide ? k_gemm_wide<T, AK, BKM, GATED>
+                               : deep ? k_gemm_mid<T, AK, BKM, GATED, 4> : k_gemm_mid<T, AK, BKM, GATED, 2>;
+    const int bytes = wide ? 4 * W_BYTES : (deep ? 4 : 2) * 2 * M_BYTES;
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e != hipSuccess) return e;
+    kernel<<<grid, wide ? 512 : 256, bytes, s>>>(a);
+    return hipGetLastError();
+}
+
 template <typename T>
 hipError_t launch_typed(const GemmArgs& a, hipStream_t s)
 {
     const Gemm& g = a.g;
-    const unsigned grid = (unsigned)(g.batches * a.splits * a.mt * a.nt);
-    const bool wide = a.tile == WT;
-    auto go = [&](void (*large)(GemmArgs), void (*wider)(GemmArgs)) {
-        void (*kernel)(GemmArgs) = wide ? wider : large;
-        const int bytes = wide ? 4 * W_BYTES : STAGES * STAGE_BYTES;
-        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize,
-                                                 bytes);
-        if (e != hipSuccess) return e;
-        kernel<<<grid, wide ? 512 : 256, bytes, s>>>(a);
-        return hipGetLastError();
-    };
-    if (g.gated) return go(k_gemm_large<T, true, true, true>, k_gemm_wide<T, true, true, true>);
-    if (g.a_kmajor && g.b_kmajor) return go(k_gemm_large<T, true, true, false>, k_gemm_wide<T, true, true, false>);
-    if (g.a_kmajor) return go(k_gemm_large<T, true, false, false>, k_gemm_wide<T, true, false, false>);
-    return go(k_gemm_large<T, false, false, false>, k_gemm_wide<T, false, false, false>);
+    if (g.gated) return launch_kernel<T, true, true, true>(a, s);
+    if (g.a_kmajor && g.b_kmajor) return launch_kernel<T, true, true, false>(a, s);
+    if (g.a_kmajor) return launch_kernel<T, true, false, false>(a, s);
+    return launch_kernel<T, false, false, false>(a, s);
 }
 
 bool pieces(const Gemm& g, const void* p, int64_t row, int64_t batch, int64_t red)
@@ -420,7 +440,7 @@ bool large_takes(const Gemm& g, bool is_a)
 // buffer loads' 31 bits, and at least a quarter of a tile.
 bool large_fits(const Gemm& g)
 {
-    if (g.dtype == ES_F32 || g.K == 0 || g.red == 0 || g.red * ((g.K - 1) / BK + 1) > 0x7FFFFFFF) return false;
+    if (g.dtype == ES_F32 || g.K == 0 || g.red == 0 || g.red * ((g.K - 1) / WK + 1) > 0x7FFFFFFF) return false;
     if (!large_takes(g, true) || !large_takes(g, false)) return false;
     // the buffers' ranges end k rows: these lie behind each other
     if ((!g.a_kmajor && g.a_row < g.M) || (!g.b_kmajor && g.b_row < g.N)) return false;
@@ -431,6 +451,10 @@ bool large_fits(const Gemm& g)
     return g.M >= 64 && g.N >= 64;
 }
 
+// 256 x 256 tiles from 192 on (three quarters of the CUs: 4096 x 4096 -> 11264 bf16
+// 334 us against 390 in smaller ones).  With at most 128 of the smaller ones, a
+// long sum is split until the CUs have one each, 8 steps at least: a split's sums
+// pass through memory twice (1024^3 in 4 splits of 4 steps 25 us, in 2 of 8 21).
 void large_plan(GemmArgs& a)
 {
     const Gemm& g = a.g;
@@ -439,16 +463,14 @@ void large_plan(GemmArgs& a)
     a.mt = (g.M - 1) / WT + 1;
     a.nt = (g.N - 1) / (g.gated ? WT / 2 : WT) + 1;
     a.kt = (g.K - 1) / WK + 1;
-    int64_t tiles = g.batches * a.mt * a.nt, steps = g.red * a.kt;
-    if (tiles < 192) {
-        a.tile = BN;
-        a.mt = (g.M - 1) / BM + 1;
-        a.nt = (g.N - 1) / (g.gated ? BN / 2 : BN) + 1;
-        a.kt = (g.K - 1) / BK + 1;
-        tiles = g.batches * a.mt * a.nt;
-        steps = g.red * a.kt;
-        if (tiles < 384 && steps >= 16) {
-            const int64_t by_tiles = (512 + tiles - 1) / tiles, by_steps = steps / 8;
+    const int64_t steps = g.red * a.kt;
+    if (g.batches * a.mt * a.nt < 192) {
+        a.tile = MT;
+        a.mt = (g.M - 1) / MT + 1;
+        a.nt = (g.N - 1) / (g.gated ? MT / 2 : MT) + 1;
+        const int64_t tiles = g.batches * a.mt * a.nt;
+        if (tiles <= 128 && steps >= 8) {
+            const int64_t by_tiles = 256 / tiles, by_steps = steps / 8;
             a.splits = (int32_t)(by_tiles < by_steps ? by_tiles : by_steps);
         }
     }
