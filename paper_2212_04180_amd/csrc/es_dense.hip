@@ -24,9 +24,9 @@ namespace esmi {
 namespace {
 
 // ---- the product ----------------------------------------------------------
-// Any type, size, stride and alignment.  Four waves make a TS x TS tile of C (TS
-// 128, or 64 where there are few tiles), (TS / 2)^2 each.  A step is 128 bytes
-// of k: fetched into registers while the step before is multiplied, then
+// Any type, size, stride and alignment.  Four waves make a TM x TN tile of C: 128
+// x 128, 64 x 64 where there are few tiles, 32 x 128 for few rows (then bound by
+// the reading of B).  A step is 128 bytes of k: fetched into registers while the step before is multiplied, then
 // staged in LDS.  An operand with k contiguous is staged row by row and read 16
 // bytes a lane; piece c of row r lies at c ^ f(r), which spreads the lanes that a
 // 16-byte read serves together ({0-3, 12-15, 20-27}, {4-11, 16-19, 28-31} and
@@ -36,7 +36,7 @@ namespace {
 // i), fp32 ones word by word.
 template <typename T, bool KMAJOR, int TS>
 struct Staged {
-    static constexpr int E = 16 / sizeof(T), KT = 128 / sizeof(T), LOADS = TS * 8 / 256;
+    static constexpr int E = 16 / sizeof(T), KT = 128 / sizeof(T), LOADS = TS * 8 / 256;  // per lane
     // fp32: rows 4 apart lie 16 banks apart
     static constexpr int ROW = KMAJOR ? 128 : TS * (int)sizeof(T) + (sizeof(T) == 4 ? 16 : 32);
     static constexpr int BYTES = (KMAJOR ? TS : KT) * ROW;
@@ -123,13 +123,14 @@ struct Staged {
     }
 };
 
-template <typename T, bool AK, bool BK, bool GATED, int TS>
+template <typename T, bool AK, bool BK, bool GATED, int TM, int TN>
 __global__ __launch_bounds__(256) void k_gemm(GemmArgs a)
 {
-    using SA = Staged<T, AK, TS>;
-    using SB = Staged<T, BK, TS>;
-    constexpr int KT = 128 / sizeof(T), HALF = TS / 2, NT = TS / 32;  // NT: 16 x 16 tiles of a wave, each way
-    constexpr int OUTS = GATED ? HALF : TS, STAGED = SA::BYTES + SB::BYTES, FINAL = 4 * EPILOGUE_LDS<NT>;
+    using SA = Staged<T, AK, TM>;
+    using SB = Staged<T, BK, TN>;
+    constexpr int KT = 128 / sizeof(T), WAVES_M = TM >= 64 ? 2 : 1, WAVES_N = 4 / WAVES_M;
+    constexpr int WM = TM / WAVES_M, WN = TN / WAVES_N, MB = WM / 16, NB = WN / 16;  // a wave's rows, columns, 16 x 16 tiles
+    constexpr int OUTS = GATED ? TN / 2 : TN, STAGED = SA::BYTES + SB::BYTES, FINAL = 4 * EPILOGUE_LDS<NB>;
     __shared__ __align__(16) unsigned char lds[STAGED > FINAL ? STAGED : FINAL];
     unsigned char *sa = lds, *sb = lds + SA::BYTES;
     const Gemm& g = a.g;
@@ -139,9 +140,9 @@ __global__ __launch_bounds__(256) void k_gemm(GemmArgs a)
     const int32_t tm = id % a.mt;
     id /= a.mt;
     const int64_t split = id % (uint32_t)a.splits, batch = id / (uint32_t)a.splits;
-    const int32_t m0 = tm * TS, n0 = tn * OUTS;
+    const int32_t m0 = tm * TM, n0 = tn * OUTS;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
-    const int wm = wave / 2, wn = wave % 2;
+    const int wm = wave / WAVES_N, wn = wave % WAVES_N;
     const int64_t steps = g.red * a.kt, first = split * a.per, last = steps - first < a.per ? steps : first + a.per;
     int64_t r = a.splits > 1 ? first / a.kt : 0;
     int32_t kt = (int32_t)(first - r * a.kt);
@@ -155,19 +156,19 @@ __global__ __launch_bounds__(256) void k_gemm(GemmArgs a)
     vb.init(static_cast<const T*>(g.b) + batch * g.b_batch + r * g.b_red, g.b_row, [&](int i, int32_t& n) -> int64_t {
         if constexpr (GATED) {
             // a wave's rows: the gates, then the others
-            const int32_t o = n0 + HALF / 2 * (i / HALF) + i % (HALF / 2);
-            return (o < g.N ? o : g.N - 1) + (i / (HALF / 2) % 2 ? (int64_t)g.N : 0);
+            const int32_t o = n0 + WN / 2 * (i / WN) + i % (WN / 2);
+            return (o < g.N ? o : g.N - 1) + (i / (WN / 2) % 2 ? (int64_t)g.N : 0);
         } else {
             n = g.N - n0 - i;
             return BK && n <= 0 ? g.N - 1 : n0 + i;
         }
     });
 
-    floatx4 acc[NT][NT];  // [m tile][n tile]
+    floatx4 acc[MB][NB];  // [m tile][n tile]
 #pragma unroll
-    for (int i = 0; i < NT; ++i)
+    for (int i = 0; i < MB; ++i)
 #pragma unroll
-        for (int j = 0; j < NT; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+        for (int j = 0; j < NB; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
     int64_t ra = 0, rb = 0;  // the reduction batch's offsets from r's
     auto fetch = [&]() {
         const int32_t k0 = kt * KT;
@@ -188,22 +189,21 @@ __global__ __launch_bounds__(256) void k_gemm(GemmArgs a)
         if (t + 1 < last) fetch();
 #pragma unroll
         for (int ks = 0; ks < 2; ++ks) {
-            uintx4 fa[NT], fb[NT];
+            uintx4 fa[MB], fb[NB];
 #pragma unroll
-            for (int i = 0; i < NT; ++i) {
-                fa[i] = SA::read(sa, HALF * wm + 16 * i, ks, lane);
-                fb[i] = SB::read(sb, HALF * wn + 16 * i, ks, lane);
-            }
+            for (int i = 0; i < MB; ++i) fa[i] = SA::read(sa, WM * wm + 16 * i, ks, lane);
 #pragma unroll
-            for (int i = 0; i < NT; ++i)
+            for (int j = 0; j < NB; ++j) fb[j] = SB::read(sb, WN * wn + 16 * j, ks, lane);
 #pragma unroll
-                for (int j = 0; j < NT; ++j) acc[i][j] = product<T>(fb[j], fa[i], acc[i][j]);
+            for (int i = 0; i < MB; ++i)
+#pragma unroll
+                for (int j = 0; j < NB; ++j) acc[i][j] = product<T>(fb[j], fa[i], acc[i][j]);
         }
     }
 
     __syncthreads();  // the staged steps make room for the epilogue
-    epilogue<T, GATED, NT, NT>(a, (int32_t)split, batch, m0 + HALF * wm, n0 + (GATED ? HALF / 2 : HALF) * wn, acc,
-                               reinterpret_cast<float*>(lds + wave * EPILOGUE_LDS<NT>), lane);
+    epilogue<T, GATED, MB, NB>(a, (int32_t)split, batch, m0 + WM * wm, n0 + (GATED ? WN / 2 : WN) * wn, acc,
+                               reinterpret_cast<float*>(lds + wave * EPILOGUE_LDS<NB>), lane);
 }
 
 // Sums of the splits and the epilogue, four outputs a thread.  Few outputs leave
@@ -369,12 +369,13 @@ void plan_path(GemmArgs& a)
     const int32_t kt = 128 / (int32_t)dtype_size(g.dtype);
     a.path = PATH_STAGED;
     a.kt = g.K ? (g.K - 1) / kt + 1 : 0;
-    a.tile = 128;
+    a.tile = g.M <= 32 && !(g.a_kmajor && g.b_kmajor) ? 32 : 128;
     for (;;) {
+        const int32_t tn = a.tile == 64 ? 64 : 128;
         a.mt = (g.M - 1) / a.tile + 1;
-        a.nt = (g.N - 1) / (g.gated ? a.tile / 2 : a.tile) + 1;
+        a.nt = (g.N - 1) / (g.gated ? tn / 2 : tn) + 1;
         // small tiles where large ones would leave CUs without work
-        if (a.tile == 64 || g.batches * a.mt * a.nt >= 512) break;
+        if (a.tile != 128 || g.batches * a.mt * a.nt >= 512) break;
         a.tile = 64;
     }
     const int64_t tiles = g.batches * a.mt * a.nt, steps = g.red * a.kt;
@@ -402,14 +403,20 @@ GemmArgs plan(const Gemm& from, void* workspace, size_t* bytes)
     return a;
 }
 
-template <typename T, int TS>
+template <typename T, int TM, int TN>
 void launch_staged(const GemmArgs& a, unsigned grid, hipStream_t s)
 {
     const Gemm& g = a.g;
-    if (g.gated) k_gemm<T, true, true, true, TS><<<grid, 256, 0, s>>>(a);
-    else if (g.a_kmajor && g.b_kmajor) k_gemm<T, true, true, false, TS><<<grid, 256, 0, s>>>(a);
-    else if (g.a_kmajor) k_gemm<T, true, false, false, TS><<<grid, 256, 0, s>>>(a);
-    else k_gemm<T, false, false, false, TS><<<grid, 256, 0, s>>>(a);
+    if (g.a_kmajor && g.b_kmajor) {
+        if constexpr (TM >= 64) {  // fewer rows have kernels of their own (es_dense_rows.hip)
+            if (g.gated) k_gemm<T, true, true, true, TM, TN><<<grid, 256, 0, s>>>(a);
+            else k_gemm<T, true, true, false, TM, TN><<<grid, 256, 0, s>>>(a);
+        }
+    } else if (g.a_kmajor) {
+        k_gemm<T, true, false, false, TM, TN><<<grid, 256, 0, s>>>(a);
+    } else {
+        k_gemm<T, false, false, false, TM, TN><<<grid, 256, 0, s>>>(a);
+    }
 }
 
 uint32_t join_quads(const Gemm& g) { return (uint32_t)(((int64_t)g.N + 3) / 4); }
@@ -422,8 +429,9 @@ hipError_t launch_typed(const GemmArgs& a, hipStream_t s)
     const unsigned grid = (unsigned)(g.batches * a.splits * a.mt * a.nt);
     hipError_t e = hipSuccess;
     if (a.path == PATH_LARGE) e = launch_large(a, s);
-    else if (a.tile == 128) launch_staged<T, 128>(a, grid, s);
-    else launch_staged<T, 64>(a, grid, s);
+    else if (a.tile == 128) launch_staged<T, 128, 128>(a, grid, s);
+    else if (a.tile == 64) launch_staged<T, 64, 64>(a, grid, s);
+    else launch_staged<T, 32, 128>(a, grid, s);
     if (e == hipSuccess) e = hipGetLastError();
     if (e != hipSuccess || a.splits == 1) return e;
     const uint32_t quads = join_quads(g);
