@@ -69,7 +69,7 @@ struct Staged {
         }
     }
     // the step whose first k has `k_left` behind it, `at` elements from the first
-    __device__ __forceinline__ void fetch(int64_t at, int32_t k_left)
+    __device__ __forceinline__ void fetch(int64_t at, int32_t k_left, bool odd)
     {
 #pragma unroll
         for (int j = 0; j < LOADS; ++j) {
@@ -78,7 +78,8 @@ struct Staged {
             if constexpr (KMAJOR) n = k_left - (c % 8) * E;
             else n = c / (TS / E) < k_left ? left[j] : 0;
             if (n >= E) {
-                __builtin_memcpy(&v[j], p[j] + at, 16);
+                if (sizeof(T) == 2 && odd) v[j] = load16_odd(p[j] + at);
+                else __builtin_memcpy(&v[j], p[j] + at, 16);
             } else {
                 T t[E];
 #pragma unroll
@@ -172,8 +173,8 @@ __global__ __launch_bounds__(256) void k_gemm(GemmArgs a)
     int64_t ra = 0, rb = 0;  // the reduction batch's offsets from r's
     auto fetch = [&]() {
         const int32_t k0 = kt * KT;
-        va.fetch(ra + (AK ? (int64_t)k0 : k0 * g.a_row), g.K - k0);
-        vb.fetch(rb + (BK ? (int64_t)k0 : k0 * g.b_row), g.K - k0);
+        va.fetch(ra + (AK ? (int64_t)k0 : k0 * g.a_row), g.K - k0, a.odd_a);
+        vb.fetch(rb + (BK ? (int64_t)k0 : k0 * g.b_row), g.K - k0, a.odd_b);
         if (++kt == a.kt) {
             kt = 0;
             ra += g.a_red;
@@ -260,9 +261,7 @@ __global__ __launch_bounds__(256) void k_gemm_join(GemmArgs a, int64_t total, ui
 
 // ---- copies in whole pieces ------------------------------------------------
 // One operand as [n][rows][ld], ld a multiple of 8 elements, zeros behind its
-// columns.  Bound by memory.  Rows of 16-bit elements at odd multiples of 2 bytes
-// are read in aligned words and shifted: 16-byte loads at such addresses run at
-// less than half the rate (rows of 4095 bf16 1.9 TB/s, of 4098 4.5).
+// columns.  Bound by memory.
 struct PackArgs {
     const uint16_t* src;
     uint16_t* dst;
@@ -279,14 +278,7 @@ __global__ __launch_bounds__(256) void k_pack(PackArgs a)
     const uint16_t* p = a.src + n * a.batch + (r - n * a.rows) * a.row + c;
     uintx4 v;
     if (left >= 8) {
-        const uintptr_t at = reinterpret_cast<uintptr_t>(p);
-        const uint32_t* w = reinterpret_cast<const uint32_t*>(at & ~(uintptr_t)3);  // words that hold the 8 elements
-        const uint32_t sh = (uint32_t)(at & 2) * 8;
-        uint32_t t[4];
-        __builtin_memcpy(t, w, 16);
-        const uint32_t last = w[sh ? 4 : 3];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = __builtin_amdgcn_alignbit(i < 3 ? t[i + 1] : last, t[i], sh);
+        v = load16_odd(p);
     } else {
         uint16_t t[8];
 #pragma unroll
@@ -322,8 +314,9 @@ size_t pack_operand(Gemm& g, bool is_a, void* base)
 
 // Whether operands are copied for the large tiles: those that they do not take as
 // they lie (both where the k of a row ends within a piece), if the staged kernel's
-// further time (about 450 TFLOP/s against 1100, measured at 8192 x 4095 x 4095:
-// forward 404 us against 218 and the copies' 50) is more than the copies'.
+// further time is more than the copies' (at 250 TFLOP/s against 1100: 512 x 4095 x
+// 4095 125 us staged, 37 from copies made in 20; 8192 x 4095 x 4095 404, 218 and 50;
+// 256 members of 255 x 257 x 255 66, 30 and 40: left as it is).
 Packing packing(const Gemm& g)
 {
     Packing p{};
@@ -337,7 +330,7 @@ Packing packing(const Gemm& g)
     if (p.a) p.a_bytes = pack_operand(h, true, reinterpret_cast<void*>(WORKSPACE_ALIGN));
     if (p.b) p.b_bytes = pack_operand(h, false, reinterpret_cast<void*>(WORKSPACE_ALIGN));
     const double flops = 2.0 * g.batches * g.red * g.M * (g.gated ? 2.0 : 1.0) * g.N * g.K;
-    const double gain = flops * (1 / 450e12 - 1 / 1100e12), cost = 2.0 * (p.a_bytes + p.b_bytes) / 4e12 + 4e-6 * (p.a + p.b);
+    const double gain = flops * (1 / 250e12 - 1 / 1100e12), cost = 2.0 * (p.a_bytes + p.b_bytes) / 4e12 + 4e-6 * (p.a + p.b);
     if (gain <= cost || !large_fits(h)) return Packing{};
     return p;
 }
@@ -360,10 +353,17 @@ hipError_t launch_pack(const Gemm& from, const Gemm& to, bool is_a, hipStream_t 
     return hipGetLastError();
 }
 
+bool odd(const Gemm& g, const void* p, int64_t row, int64_t batch, int64_t red)
+{
+    return g.dtype != ES_F32 && (reinterpret_cast<uintptr_t>(p) % 4 || row % 2 || (g.batches > 1 && batch % 2) || (g.red > 1 && red % 2));
+}
+
 // Kernel, tiles and splits of a.g
 void plan_path(GemmArgs& a)
 {
     const Gemm& g = a.g;
+    a.odd_a = odd(g, g.a, g.a_row, g.a_batch, g.a_red);
+    a.odd_b = odd(g, g.b, g.b_row, g.b_batch, g.b_red);
     if (rows_fits(g)) return rows_plan(a);
     if (large_fits(g)) return large_plan(a);
     const int32_t kt = 128 / (int32_t)dtype_size(g.dtype);

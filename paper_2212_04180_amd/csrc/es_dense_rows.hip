@@ -4,8 +4,8 @@
 // A wave owns 16 outputs: it reads 64 bytes of k of their 16 rows of w at a time,
 // 16 bytes a lane, straight from memory into the operand registers of the
 // matrix instruction (lane = row + 16 * piece is their layout), and the same
-// piece of up to 16 rows of x, which stay in the caches.  16 pieces are in
-// flight at once.  Long rows are shared by up to 16 waves of a workgroup, whose
+// piece of up to 16 rows of x, which stay in the caches.  12 to 18 pieces
+// are in flight at once.  Long rows are shared by up to 16 waves of a workgroup, whose
 // sums are added in their order through LDS.  Rows behind the last output or
 // the last row of x are read as that last one; what they give is not stored.
 #include <hip/hip_runtime.h>
@@ -38,12 +38,22 @@ __device__ __forceinline__ uintx4 piece(const T* row, int32_t k, int32_t K)
     return v;
 }
 
-template <typename T, bool GATED, int MT>
+template <typename T, bool ODD>
+__device__ __forceinline__ uintx4 whole(const T* p)
+{
+    if constexpr (ODD) return load16_odd(p);
+    uintx4 v;
+    __builtin_memcpy(&v, p, 16);
+    return v;
+}
+
+// ODD: 16-bit rows of w or x at odd multiples of 2 bytes
+template <typename T, bool GATED, int MT, bool ODD>
 __global__ __launch_bounds__(64 * MOST_WAVES) void k_rows(GemmArgs a)
 {
     __shared__ floatx4 red[MOST_WAVES][GATED ? 2 : 1][MT][64];
     const Gemm& g = a.g;
-    constexpr int E = 16 / sizeof(T), CHUNK = 4 * E, U = MT * (GATED ? 2 : 1) > 2 ? 4 : 8, NW = GATED ? 2 : 1;
+    constexpr int E = 16 / sizeof(T), CHUNK = 4 * E, U = MT == 2 ? 4 : GATED ? 6 : 8, NW = GATED ? 2 : 1;
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), q = lane / 16, l16 = lane % 16;
     const int per_tile = a.splits, tiles = (int)(blockDim.x / 64) / per_tile;  // waves a tile, tiles a workgroup
     const uint32_t groups = a.nt;
@@ -85,11 +95,11 @@ __global__ __launch_bounds__(64 * MOST_WAVES) void k_rows(GemmArgs a)
 #pragma unroll
         for (int h = 0; h < NW; ++h)
 #pragma unroll
-            for (int u = 0; u < N; ++u) __builtin_memcpy(&fw[h][u], w[h] + at + u * CHUNK, 16);
+            for (int u = 0; u < N; ++u) fw[h][u] = whole<T, ODD>(w[h] + at + u * CHUNK);
 #pragma unroll
         for (int i = 0; i < MT; ++i)
 #pragma unroll
-            for (int u = 0; u < N; ++u) __builtin_memcpy(&fx[i][u], x[i] + at + u * CHUNK, 16);
+            for (int u = 0; u < N; ++u) fx[i][u] = whole<T, ODD>(x[i] + at + u * CHUNK);
         // all of them in flight before the first is used
         __builtin_amdgcn_sched_barrier(0);
         at += N * CHUNK;
@@ -103,7 +113,7 @@ __global__ __launch_bounds__(64 * MOST_WAVES) void k_rows(GemmArgs a)
     };
     if (n0 < g.N) {
         while (c + U <= full) batch_of(std::integral_constant<int, U>{});
-        if (U == 8 && c + 4 <= full) batch_of(std::integral_constant<int, 4>{});
+        if (U > 4 && c + 4 <= full) batch_of(std::integral_constant<int, 4>{});
         if (c + 2 <= full) batch_of(std::integral_constant<int, 2>{});
         for (; c < c1; ++c) {
             const int32_t k = c * CHUNK + E * q;
@@ -144,19 +154,26 @@ __global__ __launch_bounds__(64 * MOST_WAVES) void k_rows(GemmArgs a)
     }
 }
 
-template <typename T, bool GATED>
+template <typename T, bool GATED, bool ODD>
 void launch_rows_of(const GemmArgs& a, unsigned grid, unsigned threads, hipStream_t s)
 {
-    if (a.g.M <= 16) k_rows<T, GATED, 1><<<grid, threads, 0, s>>>(a);
-    else k_rows<T, GATED, 2><<<grid, threads, 0, s>>>(a);
+    if (a.g.M <= 16) k_rows<T, GATED, 1, ODD><<<grid, threads, 0, s>>>(a);
+    else k_rows<T, GATED, 2, ODD><<<grid, threads, 0, s>>>(a);
 }
 
 template <typename T>
 hipError_t launch_typed(const GemmArgs& a, hipStream_t s)
 {
     const unsigned grid = (unsigned)(a.g.batches * a.nt), threads = 64u * a.mt;
-    if (a.g.gated) launch_rows_of<T, true>(a, grid, threads, s);
-    else launch_rows_of<T, false>(a, grid, threads, s);
+    if constexpr (sizeof(T) == 2) {
+        if (a.odd_a || a.odd_b) {
+            if (a.g.gated) launch_rows_of<T, true, true>(a, grid, threads, s);
+            else launch_rows_of<T, false, true>(a, grid, threads, s);
+            return hipGetLastError();
+        }
+    }
+    if (a.g.gated) launch_rows_of<T, true, false>(a, grid, threads, s);
+    else launch_rows_of<T, false, false>(a, grid, threads, s);
     return hipGetLastError();
 }
 
