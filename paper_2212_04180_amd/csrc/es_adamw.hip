@@ -1,7 +1,7 @@
 // es_adamw.hip -- AdamW on many tensors in one launch, gfx950.
 //
 // Bound by memory: an element takes 28 bytes with 32-bit states and gradients
-// (16 and 1/8 with 8-bit states), against about 60 instructions.  One wave owns
+// (16 and 1/8 with 8-bit states), against about 70 instructions.  One wave owns
 // 256 consecutive elements, four a lane: the loads and stores of p, m, v are
 // 16 bytes a lane, and a block of 8-bit states that shares a scale is exactly
 // one wave's, so that its new scale is one reduction across the lanes and the
@@ -42,6 +42,7 @@ struct AdamwArgs {
     Tensor t[MAX_TENSORS];
     int32_t count;
     float beta1, omb1, beta2, omb2, bc1, bc2, eps;
+    float rbc1, rsbc2;  // 1 / bc1, 1 / sqrt(bc2)
     uint32_t span;  // blocks per wave
 };
 static_assert(sizeof(AdamwArgs) <= 4096, "the table travels in the kernel's arguments");
@@ -121,10 +122,15 @@ __device__ __forceinline__ uint32_t encode4(const float x[4], float& scale)
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off));
     scale = fmaxf(top * (1.0f / F8_MAX), 0x1p-126f);
+    // x / scale correctly rounded by one residual of x times the correctly rounded
+    // reciprocal (Markstein 1990): the wave divides once, not eight times a lane.
+    // (The residual is exact for scales above 2^-90; below, a code may be the next one.)
+    const float r = 1.0f / scale;
     float q[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        q[i] = x[i] / scale;
+        const float q0 = x[i] * r;
+        q[i] = __builtin_copysignf(__builtin_fmaf(__builtin_fmaf(-q0, scale, x[i]), r, q0), x[i]);  // -0 stays
         if (ROOT && x[i] > 0.f) q[i] = fmaxf(q[i], F8_MIN);
         // at most 448 but for the division's rounding; infinities become NaN
         q[i] = __builtin_fabsf(x[i]) < __builtin_inff() ? fminf(fmaxf(q[i], -F8_MAX), F8_MAX) : __builtin_nanf("");
@@ -155,7 +161,7 @@ __global__ __launch_bounds__(256) void k_adamw(AdamwArgs a)
         const int64_t block = block0 + k, e = block * BLOCK + 4 * lane;
         if (block * BLOCK >= t.n) return;
         const int left = t.n - e >= 4 ? 4 : t.n > e ? (int)(t.n - e) : 0;
-        float p[4], g[4], m[4], v[4];
+        float p[4], g[4], m[4], v[4], q[4];
         load4(t.p + e, whole, left, p);
         load4(static_cast<const G*>(t.g) + e, whole, left, g);
         if constexpr (BITS == 32) {
@@ -170,6 +176,8 @@ __global__ __launch_bounds__(256) void k_adamw(AdamwArgs a)
             }
             store4(tm + e, whole, left, m);
             store4(tv + e, whole, left, v);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) q[i] = (m[i] / a.bc1) / (sqrtf(v[i] / a.bc2) + a.eps);
         } else {
             uint8_t* tm = static_cast<uint8_t*>(t.m);
             uint8_t* tv = static_cast<uint8_t*>(t.v);
@@ -182,6 +190,8 @@ __global__ __launch_bounds__(256) void k_adamw(AdamwArgs a)
                 v[i] = (r[i] * r[i]) * a.beta2 + (g[i] * g[i]) * a.omb2;
                 r[i] = sqrtf(v[i]);
                 if (i >= left) m[i] = r[i] = 0.f;
+                // the step itself to a few roundings: no code hangs on it
+                q[i] = m[i] * a.rbc1 * __builtin_amdgcn_rcpf(__builtin_fmaf(r[i], a.rsbc2, a.eps));
             }
             store4_codes(tm + e, whole, left, encode4<false>(m, sm));
             store4_codes(tv + e, whole, left, encode4<true>(r, sv));
@@ -192,8 +202,7 @@ __global__ __launch_bounds__(256) void k_adamw(AdamwArgs a)
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const float q = (m[i] / a.bc1) / (sqrtf(v[i] / a.bc2) + a.eps);
-            p[i] = __builtin_fmaf(-t.lr, q, p[i] * t.keep);
+            p[i] = __builtin_fmaf(-t.lr, q[i], p[i] * t.keep);
         }
         store4(t.p + e, whole, left, p);
         if (t.copy) store4(static_cast<C*>(t.copy) + e, whole, left, p);
@@ -284,6 +293,8 @@ extern "C" es_status es_adamw(const es_adamw_args* a, const es_adamw_tensor* ten
     k.omb2 = (float)(1.0 - (double)a->beta2);
     k.bc1 = (float)(1.0 - std::pow((double)a->beta1, t));
     k.bc2 = (float)(1.0 - std::pow((double)a->beta2, t));
+    k.rbc1 = (float)(1.0 / (1.0 - std::pow((double)a->beta1, t)));
+    k.rsbc2 = (float)(1.0 / std::sqrt(1.0 - std::pow((double)a->beta2, t)));
     k.eps = a->eps;
     k.span = total > (int64_t)1 << 16 ? 4 : 1;
     hipStream_t s = static_cast<hipStream_t>(hip_stream);

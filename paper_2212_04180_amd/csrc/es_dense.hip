@@ -400,6 +400,7 @@ GemmArgs plan(const Gemm& from, void* workspace, size_t* bytes)
     *bytes = pk.a_bytes + pk.b_bytes;
     if (a.path != PATH_ROWS && a.splits > 1)
         *bytes += workspace_up((size_t)4 * a.splits * g.batches * g.M * (g.gated ? 2 : 1) * (size_t)g.N);
+    *bytes += workspace_up((size_t)4 * 256 * 256 * a.tail * a.tail_splits);
     return a;
 }
 

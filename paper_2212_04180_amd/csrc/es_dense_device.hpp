@@ -149,6 +149,10 @@ struct GemmArgs {
     int32_t tile;          // staged: edge of a tile
     bool odd_a, odd_b;     // 16-bit rows at odd multiples of 2 bytes
     int64_t per;           // steps of a split
+    // 256 x 256 tiles only: the last `tail` tiles, which would leave most CUs idle
+    // at the end, are split into tail_splits parts of tail_per steps; their sums go
+    // to partial as [tail_splits][tail][256][256]
+    int32_t tail, tail_splits, tail_per;
     float* partial;        // [splits][batches][M][N or 2 N]
 };
 
@@ -272,9 +276,11 @@ __device__ __forceinline__ void wave_sync()
 // a lane finishes 8 outputs side by side and 64-column rows are stored whole;
 // straight from the accumulators the same code took 9 times the instructions
 // and a seventh of a 4096-long product's time.  lds: this wave's own.
+// part: null, or where the sums of this wave's rows and columns go instead, rows
+// of 256, a gated layer's others 128 behind its gates.
 template <typename T, bool GATED, int MB, int NB>
 __device__ __forceinline__ void epilogue(const GemmArgs& a, int32_t split, int64_t batch, int32_t m0, int32_t n0,
-                                         floatx4 (&acc)[MB][NB], float* lds, int lane)
+                                         floatx4 (&acc)[MB][NB], float* lds, int lane, float* part = nullptr)
 {
     const Gemm& g = a.g;
     constexpr int COLS = 16 * NB, PITCH = COLS + 4, OUTS = GATED ? COLS / 2 : COLS;
@@ -296,15 +302,22 @@ __device__ __forceinline__ void epilogue(const GemmArgs& a, int32_t split, int64
             const int32_t m = m0 + 32 * p + r;
             if (m >= g.M || n >= g.N) continue;
             float z[8], u[8], res[8];
-            if (a.splits == 1) load_res<T, 8>(a, batch, m, n, res);
+            if (a.splits == 1 && !part) load_res<T, 8>(a, batch, m, n, res);
             const float* from = lds + r * PITCH + col;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 z[e] = from[e];
                 u[e] = GATED ? from[e + COLS / 2] : 0.f;
             }
-            if (a.splits > 1) store_partial<GATED, 8>(a, split, batch, m, n, z, u);
-            else finish<T, GATED, 8>(a, batch, m, n, z, u, bz, bu, res);
+            if (part) {
+                float* to = part + (32 * p + r) * 256 + col;
+                store_run<float, 8>(to, 8, z);
+                if constexpr (GATED) store_run<float, 8>(to + 128, 8, u);
+            } else if (a.splits > 1) {
+                store_partial<GATED, 8>(a, split, batch, m, n, z, u);
+            } else {
+                finish<T, GATED, 8>(a, batch, m, n, z, u, bz, bu, res);
+            }
         }
         wave_sync();
     }

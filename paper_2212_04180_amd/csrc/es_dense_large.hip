@@ -108,12 +108,16 @@ struct Operand {
     }
 };
 
-// Workgroups are dealt to the 8 XCDs in turn: consecutive tiles go to one XCD, in
-// blocks of 4 m tiles, so that the tiles in flight on an XCD share rows in its L2.
+// Workgroups are dealt to the 8 XCDs in turn: consecutive tiles of the `count` go
+// to one XCD,
+__device__ __forceinline__ uint32_t on_one_xcd(uint32_t id, uint32_t count)
+{
+    const uint32_t per = count / 8, rest = count % 8, x = id % 8;
+    return x * per + (x < rest ? x : rest) + id / 8;
+}
+// in blocks of 4 m tiles, so that the tiles in flight on an XCD share rows in its L2.
 __device__ __forceinline__ void tile_of(uint32_t id, uint32_t mt, uint32_t nt, int32_t& tm, int32_t& tn)
 {
-    const uint32_t count = mt * nt, per = count / 8, rest = count % 8, x = id % 8;
-    id = x * per + (x < rest ? x : rest) + id / 8;
     constexpr uint32_t G = 4;
     const uint32_t group = id / (G * nt), in = id % (G * nt), first = group * G, rows = mt - first < G ? mt - first : G;
     tm = __builtin_amdgcn_readfirstlane(first + in % rows);
@@ -135,7 +139,7 @@ __global__ __launch_bounds__(256, 2) void k_gemm_mid(GemmArgs a)
     constexpr int OUTS = GATED ? MT / 2 : MT;  // outputs of a tile
     const uint32_t tiles = (uint32_t)a.mt * a.nt, outer = blockIdx.x / tiles;
     int32_t tm, tn;
-    tile_of(blockIdx.x % tiles, a.mt, a.nt, tm, tn);
+    tile_of(on_one_xcd(blockIdx.x % tiles, tiles), a.mt, a.nt, tm, tn);
     const int32_t split = __builtin_amdgcn_readfirstlane(outer % a.splits);
     const int64_t batch = (uint32_t)__builtin_amdgcn_readfirstlane(outer / a.splits);
     const int32_t m0 = tm * MT, n0 = tn * OUTS;
@@ -260,15 +264,29 @@ __global__ __launch_bounds__(512, 2) void k_gemm_wide(GemmArgs a)
     extern __shared__ __align__(1024) unsigned char lds[];
     const Gemm& g = a.g;
     constexpr int OUTS = GATED ? WT / 2 : WT;
-    const uint32_t tiles = (uint32_t)a.mt * a.nt, outer = blockIdx.x / tiles;
-    int32_t tm, tn;
-    tile_of(blockIdx.x % tiles, a.mt, a.nt, tm, tn);
+    // A launch with a tail starts with half of its parts, so that those CUs are out of
+    // step with the others: the epilogues' stores then meet other tiles' products.
+    const uint32_t tiles = (uint32_t)a.mt * a.nt, full = tiles - a.tail, ahead = a.tail * (a.tail_splits / 2);
+    uint32_t id = blockIdx.x, outer = 0;
+    int32_t tm, tn, part = -1;
+    if (a.tail == 0) {
+        outer = id / tiles;
+        id = on_one_xcd(id % tiles, tiles);
+    } else if (id >= ahead && id < ahead + full) {
+        id = on_one_xcd(id - ahead, full);
+    } else {
+        part = __builtin_amdgcn_readfirstlane(id < ahead ? id : id - full);
+        id = full + part % a.tail;
+    }
+    tile_of(id, a.mt, a.nt, tm, tn);
     const int32_t split = __builtin_amdgcn_readfirstlane(outer % a.splits);
     const int64_t batch = (uint32_t)__builtin_amdgcn_readfirstlane(outer / a.splits);
     const int32_t m0 = tm * WT, n0 = tn * OUTS;
-    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64); const int group = wave / 4, wm = group, wn = wave % 4;
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    const int group = wave / 4, wm = group, wn = wave % 4;
     const int32_t steps = (int32_t)g.red * a.kt;  // below 2^31
-    const int32_t per = (int32_t)a.per, first = split * per, count = steps - first < per ? steps - first : per;
+    const int32_t per = part < 0 ? (int32_t)a.per : a.tail_per;
+    const int32_t first = (part < 0 ? split : part / a.tail) * per, count = steps - first < per ? steps - first : per;
 
     using OA = Operand<AK, WT, WK, 512>;
     using OB = Operand<BKM, WT, WK, 512>;
@@ -286,7 +304,7 @@ __global__ __launch_bounds__(512, 2) void k_gemm_wide(GemmArgs a)
         ob.init(g.b_row, [&](int i) -> int64_t { return n0 + i < g.N ? (BKM ? i : n0 + i) : -1; });
     }
     int32_t kt = first;
-    if (a.splits > 1 && g.red > 1) {
+    if (first > 0 && g.red > 1) {
         const int32_t r = __builtin_amdgcn_readfirstlane((uint32_t)first / (uint32_t)a.kt);
         kt = first - r * a.kt;
         pa += r * g.a_red;
@@ -391,22 +409,59 @@ __global__ __launch_bounds__(512, 2) void k_gemm_wide(GemmArgs a)
     arrived();
     __syncthreads();  // the buffers serve the epilogue
     epilogue<T, GATED, 8, 4>(a, split, batch, m0 + 128 * wm, n0 + (GATED ? 32 : 64) * wn, acc,
-                             reinterpret_cast<float*>(lds + wave * EPILOGUE_LDS<4>), lane);
+                             reinterpret_cast<float*>(lds + wave * EPILOGUE_LDS<4>), lane,
+                             part < 0 ? nullptr : a.partial + ((int64_t)part * WT + 128 * wm) * WT + (GATED ? 32 : 64) * wn);
 }
 static_assert(8 * EPILOGUE_LDS<4> <= 4 * W_BYTES, "the epilogue's rows fit the buffers");
+
+// The tail's sums and their epilogue, four outputs a thread
+template <typename T, bool GATED>
+__global__ __launch_bounds__(256) void k_tail_join(GemmArgs a)
+{
+    const Gemm& g = a.g;
+    constexpr int OUTS = GATED ? WT / 2 : WT, PER = WT * OUTS / 4 / 256;  // workgroups a tile
+    const uint32_t tile = blockIdx.x / PER, at = (blockIdx.x % PER) * 256 + threadIdx.x;
+    const int32_t row = at / (OUTS / 4), col = at % (OUTS / 4) * 4;
+    int32_t tm, tn;
+    tile_of((uint32_t)a.mt * a.nt - a.tail + tile, a.mt, a.nt, tm, tn);
+    const int32_t m = tm * WT + row, n = tn * OUTS + col;
+    if (m >= g.M || n >= g.N) return;
+    float z[4] = {}, u[4] = {}, bz[4], bu[4], r[4];
+    load_bias<T, GATED, 4>(g, 0, n, bz, bu);
+    load_res<T, 4>(a, 0, m, n, r);
+    const float* p = a.partial + ((int64_t)tile * WT + row) * WT + col;
+#pragma unroll 2
+    for (int32_t s = 0; s < a.tail_splits; ++s, p += (int64_t)a.tail * WT * WT) {
+        float v[4];
+        load_run<float, 4>(p, 4, v);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) z[i] += v[i];
+        if constexpr (GATED) {
+            load_run<float, 4>(p + WT / 2, 4, v);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) u[i] += v[i];
+        }
+    }
+    finish<T, GATED, 4>(a, 0, m, n, z, u, bz, bu, r);
+}
 
 template <typename T, bool AK, bool BKM, bool GATED>
 hipError_t launch_kernel(const GemmArgs& a, hipStream_t s)
 {
-    const unsigned grid = (unsigned)(a.g.batches * a.splits * a.mt * a.nt);
+    const unsigned grid = (unsigned)(a.g.batches * a.splits * a.mt * a.nt + (int64_t)a.tail * (a.tail_splits - 1));
     const bool wide = a.tile == WT, deep = grid <= 256;
     void (*kernel)(GemmArgs) = wide ? k_gemm_wide<T, AK, BKM, GATED>
                                : deep ? k_gemm_mid<T, AK, BKM, GATED, 4> : k_gemm_mid<T, AK, BKM, GATED, 2>;
     const int bytes = wide ? 4 * W_BYTES : (deep ? 4 : 2) * 2 * M_BYTES;
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (e != hipSuccess) return e;
     kernel<<<grid, wide ? 512 : 256, bytes, s>>>(a);
-    return hipGetLastError();
+    e = hipGetLastError();
+    if (e == hipSuccess && a.tail) {
+        k_tail_join<T, GATED><<<(unsigned)a.tail * (WT * WT / (GATED ? 2 : 1) / 1024), 256, 0, s>>>(a);
+        e = hipGetLastError();
+    }
+    return e;
 }
 
 template <typename T>
@@ -476,6 +531,22 @@ void large_plan(GemmArgs& a)
     }
     a.per = (steps + a.splits - 1) / a.splits;
     a.splits = (int32_t)((steps + a.per - 1) / a.per);
+    // At most half a round of tiles behind full ones: in parts they take a part of a
+    // round (1.6 us a step), their sums go through memory once more (bf16, 4096 long:
+    // 4352 rows to 4096 outputs, 16 tiles over, 186 -> 131 us; 8192 to 4608, 64 over,
+    // 288 -> 257; 8192 to 11264, 128 over, 647 -> 606).
+    const int64_t tiles = (int64_t)a.mt * a.nt, rest = tiles % 256;
+    if (a.tile == WT && g.batches == 1 && tiles > 256 && rest > 0 && rest <= 128) {
+        int64_t parts = 256 / rest;
+        if (parts > steps / 8) parts = steps / 8;
+        const double saved = steps * 1.6e-6 * (1.0 - 1.0 / (double)parts);
+        const double cost = 2.0 * rest * parts * WT * WT * 4 / 4.5e12 + 5e-6;
+        if (parts >= 2 && saved > cost) {
+            a.tail_per = (int32_t)((steps + parts - 1) / parts);
+            a.tail_splits = (int32_t)((steps + a.tail_per - 1) / a.tail_per);
+            a.tail = (int32_t)rest;
+        }
+    }
 }
 
 hipError_t launch_large(const GemmArgs& a, hipStream_t s)

@@ -112,6 +112,14 @@ def test_many_tiles(dtype, members, rows, k, f):
         _check(24, dtype, members, rows, k, f, "none", shared_w=True)
 
 
+@pytest.mark.parametrize("dtype,rows,k,f", [(BF, 4104, 1096, 4096), (HF, 4360, 1024, 4088), (BF, 4104, 4096, 4104)])
+def test_tiles_left_over(dtype, rows, k, f):
+    """A few tiles behind full rounds of the chip's: their sums are made in parts."""
+    _check(28, dtype, None, rows, k, f, "silu", residual=True)
+    if k < 2000:
+        _check(29, dtype, None, rows, k, f // 2, "gelu", gated=True)
+
+
 @pytest.mark.parametrize("dtype", [BF, HF])
 @pytest.mark.parametrize("members,rows,k,f,kw", [
     (None, 4100, 1031, 2051, {}), (None, 2049, 2052, 2047, {}), (3, 2050, 1031, 1029, {}), (3, 1401, 1031, 2051, dict(shared_w=True)),
