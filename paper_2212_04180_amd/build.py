@@ -9,6 +9,7 @@ import os
 import shutil
 import subprocess
 import sys
+from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -54,15 +55,20 @@ def build_probe(cc: str, verbose: bool = False) -> str:
 
 def build(verbose: bool = False) -> str:
     cc = hipcc()
-    build_probe(cc, verbose)
-    objs = []
-    for src in SOURCES:
-        obj = os.path.join(CSRC, src + ".o")
-        cmd = [cc, *compile_flags(), "-c", "-x", "hip", os.path.join(CSRC, src), "-o", obj]
+    objs = [os.path.join(CSRC, src + ".o") for src in SOURCES]
+    cmds = [[cc, *compile_flags(), "-c", "-x", "hip", os.path.join(CSRC, src), "-o", obj] for src, obj in zip(SOURCES, objs)]
+
+    def run(cmd):
         if verbose:
             print(" ".join(cmd), flush=True)
         subprocess.run(cmd, check=True, stderr=None if verbose else subprocess.PIPE)
-        objs.append(obj)
+
+    # one compiler per source, a handful at once (each takes about 1 GB)
+    with ThreadPoolExecutor(max_workers=min(6, os.cpu_count() or 1)) as pool:
+        probe = pool.submit(build_probe, cc, verbose)
+        for done in [pool.submit(run, cmd) for cmd in cmds]:
+            done.result()
+        probe.result()
     tmp = LIB + ".tmp%d" % os.getpid()
     cmd = [cc, f"--offload-arch={ARCH}", "-shared", "-fPIC", "-o", tmp, *objs]
     if verbose:

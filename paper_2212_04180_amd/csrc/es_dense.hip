@@ -578,11 +578,12 @@ bool gemm_too_large(const Gemm& g)
            (a.splits > 1 && (__int128)g.batches * g.M * join_quads(g) / 256 >= most);
 }
 
-hipError_t launch_gemm(const Gemm& g, void* workspace, hipStream_t s)
+hipError_t launch_gemm(const Gemm& g, void* workspace, size_t bytes, hipStream_t s)
 {
     size_t n = 0;
     const GemmArgs a = plan(g, workspace, &n);
-    hipError_t e = hipSuccess;
+    hipError_t e = n <= bytes ? hipSuccess : hipErrorInvalidValue;
+    if (e != hipSuccess) return e;
     if (a.g.a != g.a) e = launch_pack(g, a.g, true, s);
     if (e == hipSuccess && a.g.b != g.b) e = launch_pack(g, a.g, false, s);
     if (e != hipSuccess) return e;

@@ -45,7 +45,8 @@ struct Gemm {
 // Bytes that the product keeps between its launches: copies of operands in whole
 // pieces, partial sums where its reduction is split (0: one launch).
 size_t gemm_workspace(const Gemm& g);
-hipError_t launch_gemm(const Gemm& g, void* workspace, hipStream_t s);
+// hipErrorInvalidValue where `bytes` is less than gemm_workspace gives
+hipError_t launch_gemm(const Gemm& g, void* workspace, size_t bytes, hipStream_t s);
 bool gemm_too_large(const Gemm& g);  // more workgroups than a launch holds
 
 // dz = dy act'(pre) (or both halves of a gated layer) in the type, rows of

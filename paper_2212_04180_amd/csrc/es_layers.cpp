@@ -126,7 +126,7 @@ es_status forward(const es_dense_args* a, bool gated, const char* who, void* ws,
     if (bytes < want) return init_fail(ES_ERR_ARG, "the workspace is too small", who);
     if (want && reinterpret_cast<uintptr_t>(ws) % kAlign) return init_fail(ES_ERR_ARG, "the workspace is not aligned", who);
     if (empty) return ES_OK;
-    const hipError_t e = launch_gemm(g, ws, static_cast<hipStream_t>(stream));
+    const hipError_t e = launch_gemm(g, ws, bytes, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? ES_OK : init_fail(ES_ERR_HIP, hipGetErrorString(e), who);
 }
 
@@ -182,13 +182,15 @@ BackwardPlan plan_backward(const es_dense_grad_args& a, bool gated)
     p.z.ldz = ldz;
     const int64_t z_row = p.store_dz ? ldz : a.dy.row, z_member = p.store_dz ? B * ldz : a.dy.member;
 
+    // The plans (and so the workspace) go by addresses: dz will start the workspace.
+    const void* z = p.store_dz ? reinterpret_cast<const void*>(kAlign) : a.dy.p;
     Gemm g{};
     g.dtype = g.c_dtype = a.dtype;
     g.act = ES_ACT_NONE;
     // dx[i][k] = sum_o dz[i][o] w[o][k]
     p.dx = g;
     p.dx.M = (int32_t)B; p.dx.N = (int32_t)a.in; p.dx.K = (int32_t)wide;
-    p.dx.a = a.dy.p; p.dx.a_row = z_row; p.dx.a_kmajor = true; p.dx.a_padded = p.store_dz;
+    p.dx.a = z; p.dx.a_row = z_row; p.dx.a_kmajor = true; p.dx.a_padded = p.store_dz;
     p.dx.b = a.w.p; p.dx.b_row = a.w.row; p.dx.b_kmajor = false;
     p.dx.c = a.dx.p; p.dx.c_row = a.dx.row; p.dx.c_batch = a.dx.member;
     if (sum_dx) {
@@ -203,7 +205,7 @@ BackwardPlan plan_backward(const es_dense_grad_args& a, bool gated)
     // dw[o][k] = sum_i dz[i][o] x[i][k]
     p.dw = g;
     p.dw.M = (int32_t)wide; p.dw.N = (int32_t)a.in; p.dw.K = (int32_t)B;
-    p.dw.a = a.dy.p; p.dw.a_row = z_row; p.dw.a_kmajor = false; p.dw.a_padded = p.store_dz;
+    p.dw.a = z; p.dw.a_row = z_row; p.dw.a_kmajor = false; p.dw.a_padded = p.store_dz;
     p.dw.b = a.x.p; p.dw.b_row = a.x.row; p.dw.b_kmajor = false;
     p.dw.c = a.dw.p; p.dw.c_row = a.dw.row; p.dw.c_batch = a.dw.member;
     if (sum_dw) {
@@ -259,8 +261,8 @@ es_status backward(const es_dense_grad_args* a, bool gated, const char* who, voi
         e = launch_bias_grad(a->dtype, sums, sum ? 1 : a->members, sum ? a->members * p.chunks : p.chunks, p.wide, a->db.p,
                              a->db.member, s);
     }
-    if (e == hipSuccess && p.do_dx) e = launch_gemm(p.dx, partial, s);
-    if (e == hipSuccess && p.do_dw) e = launch_gemm(p.dw, partial, s);
+    if (e == hipSuccess && p.do_dx) e = launch_gemm(p.dx, partial, p.partial_bytes, s);
+    if (e == hipSuccess && p.do_dw) e = launch_gemm(p.dw, partial, p.partial_bytes, s);
     return e == hipSuccess ? ES_OK : init_fail(ES_ERR_HIP, hipGetErrorString(e), who);
 }
 

@@ -304,7 +304,7 @@ def adamw(params, grads, m, v, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, weigh
     cols.append(_tensors("copies", copies, n, cdt, device, sizes) if copies is not None else [0] * n)
     cols.append(sizes)
     for name, value in (("lr", lr), ("weight_decay", weight_decay)):
-        each = [float(value)] * n if isinstance(value, (int, float)) else [float(e) for e in value]
+        each = [float(e) for e in value] if isinstance(value, (list, tuple)) else [float(value)] * n
         if len(each) != n:
             raise ValueError(f"{name}: one number, or one per parameter")
         cols.append(each)

@@ -228,6 +228,18 @@ def test_output_in_32_bits_and_in_place_residual():
             L.check("gated fp32", h, v, e)
 
 
+@pytest.mark.parametrize("k,f", [(1031, 2051), (1032, 2056), (1024, 2048)])
+def test_gradients_of_an_odd_address(k, f):
+    """dy at an odd address with an activation: what the products read is dz, in the workspace."""
+    P = _P()
+    x, w, b, _, dy = _case(30, BF, None, 4100, k, f, "tanh")
+    pre = P.dense(x, w, b, act="tanh", keep_pre=True)[1]
+    moved = torch.empty(dy.numel() + 1, dtype=BF, device="cuda")[1:].view(dy.shape)
+    moved.copy_(dy)
+    for name, got, (v, bound) in zip(("dx", "dw", "db"), P.dense_backward(moved, x, w, pre, act="tanh"), L.backward(dy, x, w, pre, "tanh")):
+        L.check(name, got, v, bound)
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 def test_infinities_and_nan_stay_in_their_rows(dtype):
     P = _P()
@@ -355,8 +367,9 @@ def test_captured_and_replayed():
     """Two graphs of forward and gradients, replayed in turn with eager work between, like the eager calls."""
     P = _P()
     graphs = []
-    for seed, dtype, rows in ((17, BF, 48), (18, SF, 33)):
-        x, w, b, _, dy = _case(seed, dtype, None, rows, 1024, 64, "gelu")
+    # split sums, fp32, the large tiles with parts, copies of ragged operands
+    for seed, dtype, rows, k, f in ((17, BF, 48, 1024, 64), (18, SF, 33, 1024, 64), (19, HF, 4360, 1024, 4088), (20, BF, 2051, 2047, 2053)):
+        x, w, b, _, dy = _case(seed, dtype, None, rows, k, f, "gelu")
 
         def step(x=x, w=w, b=b, dy=dy):
             y, pre = P.dense(x, w, b, act="gelu", keep_pre=True)
