@@ -245,17 +245,18 @@ __global__ __launch_bounds__(256, 2) void k_gemm_mid(GemmArgs a)
 static_assert(4 * EPILOGUE_LDS<4> <= 2 * 2 * M_BYTES, "the epilogue's rows fit the buffers");
 
 // 256 x 256 tiles for products that fill the chip with them.  Eight waves, 128 x
-// 64 each, in two groups of one wave a SIMD, half a step of 32 k apart: while
-// one group multiplies (32 products, 512 cycles) and issues loads in between, the
-// other reads its next fragments; a barrier ends each such phase.  A step is 64
-// k: whole 128-byte lines of a k-major operand.  Two buffers of 64 KB; the loads
-// of step t + 1 are issued once both groups have read step t - 1:
-//   phase     4t        4t + 1    4t + 2   4t + 3   4t + 4
-//   group 0   read 0    mul 0, l  read 1   mul 1    read 0 of t + 1
-//   group 1   mul 1, l  read 0    mul 0    read 1   mul 1, l
-//   (l: loads of t + 1, all there after 4t + 3)
-// 8192 x 4096 x 4096 bf16 209 us, 1315 TFLOP/s; the products alone take 138, with
-// the fragments' reads 155, the loads alone 137: reads and loads share the LDS.
+// 64 each, in two groups of one wave a SIMD, a phase apart: while one group
+// multiplies a step of 64 k (64 products, 1024 cycles, at raised priority), the
+// other reads its next fragments; a barrier ends each phase.  A step's rows of a
+// k-major operand are whole 128-byte lines.  Two buffers of 64 KB; the loads of
+// step t + 1 are issued once both groups have read step t - 1:
+//   phase     2t        2t + 1     2t + 2
+//   group 0   read t, l multiply t read t + 1
+//   group 1   mul., l   read t     multiply t, l
+//   (l: loads of t + 1, all there after 2t + 1; in group 1 between the products)
+// 8192 x 4096 x 4096 bf16 201 us, 1370 TFLOP/s (phases of 32 k 204, without the
+// priority 221); of an earlier form at 209 the products alone took 138, with the
+// fragments' reads 155, the loads alone 137: reads and loads share the LDS.
 constexpr int WT = 256, WK = 64, W_BYTES = WT * WK * 2;  // of one operand's buffer
 
 template <typename T, bool AK, bool BKM, bool GATED>
@@ -327,20 +328,25 @@ __global__ __launch_bounds__(512, 2) void k_gemm_wide(GemmArgs a)
     for (int i = 0; i < 8; ++i)
 #pragma unroll
         for (int j = 0; j < 4; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
-    uintx4 fa[8], fb[4];
-    auto read = [&](int32_t t, int ks) {
+    uintx4 fa[2][8], fb[2][4];
+    auto read = [&](int32_t t) {
         const unsigned char* from = lds + (t & 1) * 2 * W_BYTES;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) fb[j] = OB::read(from + W_BYTES, 64 * wn, j, ks, lane);
+        for (int ks = 0; ks < 2; ++ks) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) fa[i] = OA::read(from, 128 * wm, i, ks, lane);
+            for (int j = 0; j < 4; ++j) fb[ks][j] = OB::read(from + W_BYTES, 64 * wn, j, ks, lane);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) fa[ks][i] = OA::read(from, 128 * wm, i, ks, lane);
+        }
     };
     auto multiply = [&]() {
         __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+        for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) acc[i][j] = product<T>(fb[j], fa[i], acc[i][j]);
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) acc[i][j] = product<T>(fb[ks][j], fa[ks][i], acc[i][j]);
         __builtin_amdgcn_s_setprio(0);
     };
     // the same with the loads of step t in between
@@ -356,13 +362,15 @@ __global__ __launch_bounds__(512, 2) void k_gemm_wide(GemmArgs a)
         }
         __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            if (i % 2 == 0) oa.load(i / 2, ba, g.a_row, left, to);
-            else ob.load(i / 2, bb, g.b_row, left, to + W_BYTES);
+        for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) acc[i][j] = product<T>(fb[j], fa[i], acc[i][j]);
-            __builtin_amdgcn_sched_barrier(0);
-        }
+            for (int i = 0; i < 8; ++i) {
+                if (i % 4 == 0) oa.load(2 * ks + i / 4, ba, g.a_row, left, to);
+                else if (i % 4 == 2) ob.load(2 * ks + i / 4, bb, g.b_row, left, to + W_BYTES);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) acc[i][j] = product<T>(fb[ks][j], fa[ks][i], acc[i][j]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
         __builtin_amdgcn_s_setprio(0);
     };
     // ends a phase: what this wave has read is in its registers
@@ -380,11 +388,9 @@ __global__ __launch_bounds__(512, 2) void k_gemm_wide(GemmArgs a)
     phase();
     if (group == 0) {
         for (int32_t t = 0; t < count; ++t) {
-            read(t, 0);
-            phase();
-            multiply_fetch(t + 1);
-            phase();
-            read(t, 1);
+            read(t);
+            __builtin_amdgcn_sched_barrier(0);
+            fetch(t + 1);
             phase();
             multiply();
             arrived();
@@ -395,11 +401,7 @@ __global__ __launch_bounds__(512, 2) void k_gemm_wide(GemmArgs a)
         fetch(1);
         phase();
         for (int32_t t = 0; t < count; ++t) {
-            read(t, 0);
-            phase();
-            multiply();
-            phase();
-            read(t, 1);
+            read(t);
             arrived();
             phase();
             multiply_fetch(t + 2);
