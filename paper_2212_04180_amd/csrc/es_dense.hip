@@ -203,7 +203,7 @@ __global__ __launch_bounds__(256) void k_gemm(GemmArgs a)
     }
 
     __syncthreads();  // the staged steps make room for the epilogue
-    epilogue<T, GATED, MB, NB>(a, (int32_t)split, batch, m0 + WM * wm, n0 + (GATED ? WN / 2 : WN) * wn, acc,
+    epilogue<T, GATED, MB, NB, TM == 128>(a, (int32_t)split, batch, m0 + WM * wm, n0 + (GATED ? WN / 2 : WN) * wn, acc,
                                reinterpret_cast<float*>(lds + wave * EPILOGUE_LDS<NB>), lane);
 }
 

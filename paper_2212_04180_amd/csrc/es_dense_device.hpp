@@ -172,14 +172,26 @@ __device__ __forceinline__ void load_run(const T* p, int32_t left, float out[W])
     for (int i = 0; i < W; ++i) out[i] = widen(t[i]);
 }
 
-template <typename T, int W>
+// STREAM: past the caches.  (Chosen at compile time: the compiler joins the two
+// stores of a branch into a plain one.)
+template <typename T, int W, bool STREAM = false>
 __device__ __forceinline__ void store_run(T* p, int32_t left, const float v[W])
 {
     T t[W];
 #pragma unroll
     for (int i = 0; i < W; ++i) t[i] = (T)v[i];
     if (left >= W) {
-        __builtin_memcpy(p, t, W * sizeof(T));
+        if constexpr (STREAM) {
+            typedef uint32_t piece __attribute__((ext_vector_type(4), aligned(2)));
+#pragma unroll
+            for (int i = 0; i < W * (int)sizeof(T) / 16; ++i) {
+                piece q;
+                __builtin_memcpy(&q, t + 16 / sizeof(T) * i, 16);
+                __builtin_nontemporal_store(q, reinterpret_cast<piece*>(p + 16 / sizeof(T) * i));
+            }
+        } else {
+            __builtin_memcpy(p, t, W * sizeof(T));
+        }
     } else {
 #pragma unroll
         for (int i = 0; i < W; ++i)
@@ -201,7 +213,7 @@ __device__ __forceinline__ void load_res(const GemmArgs& a, int64_t batch, int64
 
 // Bias, activation, gate and residual of W consecutive outputs from column n
 // of row m, rounded and stored.  bz, bu: their biases, r: the residual.
-template <typename T, bool GATED, int W>
+template <typename T, bool GATED, int W, bool STREAM = false>
 __device__ __forceinline__ void finish(const GemmArgs& a, int64_t batch, int64_t m, int32_t n, float z[W], float u[W],
                                        const float bz[W], const float bu[W], const float r[W])
 {
@@ -216,8 +228,8 @@ __device__ __forceinline__ void finish(const GemmArgs& a, int64_t batch, int64_t
     }
     if (g.pre) {
         T* pre = static_cast<T*>(g.pre) + batch * g.pre_batch + m * g.pre_row + n;
-        store_run<T, W>(pre, left, z);
-        if constexpr (GATED) store_run<T, W>(pre + g.N, left, u);
+        store_run<T, W, STREAM>(pre, left, z);
+        if constexpr (GATED) store_run<T, W, STREAM>(pre + g.N, left, u);
     }
     activate<FAST, false, W>(g.act, z, nullptr);
     if constexpr (GATED) {
@@ -229,8 +241,8 @@ __device__ __forceinline__ void finish(const GemmArgs& a, int64_t batch, int64_t
         for (int i = 0; i < W; ++i) z[i] += r[i];
     }
     const int64_t at = batch * g.c_batch + m * g.c_row + n;
-    if (g.c_dtype == ES_F32) store_run<float, W>(static_cast<float*>(g.c) + at, left, z);
-    else store_run<T, W>(static_cast<T*>(g.c) + at, left, z);
+    if (g.c_dtype == ES_F32) store_run<float, W, STREAM>(static_cast<float*>(g.c) + at, left, z);
+    else store_run<T, W, STREAM>(static_cast<T*>(g.c) + at, left, z);
 }
 
 template <typename T, bool GATED, int W>
@@ -276,9 +288,12 @@ __device__ __forceinline__ void wave_sync()
 // a lane finishes 8 outputs side by side and 64-column rows are stored whole;
 // straight from the accumulators the same code took 9 times the instructions
 // and a seventh of a 4096-long product's time.  lds: this wave's own.
+// STREAM: for launches whose outputs are more than the L2s hold (8 of 4 MB): stored
+// past them they leave the operands' rows there (8192 x 4096 -> 11264 bf16 with its
+// pre 711 -> 645 us).
 // part: null, or where the sums of this wave's rows and columns go instead, rows
 // of 256, a gated layer's others 128 behind its gates.
-template <typename T, bool GATED, int MB, int NB>
+template <typename T, bool GATED, int MB, int NB, bool STREAM>
 __device__ __forceinline__ void epilogue(const GemmArgs& a, int32_t split, int64_t batch, int32_t m0, int32_t n0,
                                          floatx4 (&acc)[MB][NB], float* lds, int lane, float* part = nullptr)
 {
@@ -316,7 +331,7 @@ __device__ __forceinline__ void epilogue(const GemmArgs& a, int32_t split, int64
             } else if (a.splits > 1) {
                 store_partial<GATED, 8>(a, split, batch, m, n, z, u);
             } else {
-                finish<T, GATED, 8>(a, batch, m, n, z, u, bz, bu, res);
+                finish<T, GATED, 8, STREAM>(a, batch, m, n, z, u, bz, bu, res);
             }
         }
         wave_sync();

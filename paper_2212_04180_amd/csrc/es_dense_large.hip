@@ -239,7 +239,7 @@ __global__ __launch_bounds__(256, 2) void k_gemm_mid(GemmArgs a)
     }
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     __syncthreads();  // the buffers serve the epilogue
-    epilogue<T, GATED, 4, 4>(a, split, batch, m0 + 64 * wm, n0 + (GATED ? 32 : 64) * wn, acc,
+    epilogue<T, GATED, 4, 4, false>(a, split, batch, m0 + 64 * wm, n0 + (GATED ? 32 : 64) * wn, acc,
                              reinterpret_cast<float*>(lds + wave * EPILOGUE_LDS<4>), lane);
 }
 static_assert(4 * EPILOGUE_LDS<4> <= 2 * 2 * M_BYTES, "the epilogue's rows fit the buffers");
@@ -410,7 +410,7 @@ __global__ __launch_bounds__(512, 2) void k_gemm_wide(GemmArgs a)
     }
     arrived();
     __syncthreads();  // the buffers serve the epilogue
-    epilogue<T, GATED, 8, 4>(a, split, batch, m0 + 128 * wm, n0 + (GATED ? 32 : 64) * wn, acc,
+    epilogue<T, GATED, 8, 4, true>(a, split, batch, m0 + 128 * wm, n0 + (GATED ? 32 : 64) * wn, acc,
                              reinterpret_cast<float*>(lds + wave * EPILOGUE_LDS<4>), lane,
                              part < 0 ? nullptr : a.partial + ((int64_t)part * WT + 128 * wm) * WT + (GATED ? 32 : 64) * wn);
 }
