@@ -521,7 +521,12 @@ void large_plan(GemmArgs& a)
     a.nt = (g.N - 1) / (g.gated ? WT / 2 : WT) + 1;
     a.kt = (g.K - 1) / WK + 1;
     const int64_t steps = g.red * a.kt;
-    if (g.batches * a.mt * a.nt < 192) {
+    const int64_t wides = (int64_t)a.mt * a.nt;
+    // no wider than the smaller tiles: half of the larger ones, or more, would be padding
+    // (128 rows of 4096 to 49152 bf16 127 us, 99 in smaller tiles; 64 of 2048 to 131072 147, 137)
+    const bool thin = g.M <= MT || g.N <= (g.gated ? MT / 2 : MT);
+    const bool all_parts = !thin && g.batches == 1 && wides >= 48 && wides <= 128 && steps >= 160;
+    if (thin || (g.batches * a.mt * a.nt < 192 && !all_parts)) {
         a.tile = MT;
         a.mt = (g.M - 1) / MT + 1;
         a.nt = (g.N - 1) / (g.gated ? MT / 2 : MT) + 1;
@@ -536,14 +541,17 @@ void large_plan(GemmArgs& a)
     // At most half a round of tiles behind full ones: in parts they take a part of a
     // round (1.6 us a step), their sums go through memory once more (bf16, 4096 long:
     // 4352 rows to 4096 outputs, 16 tiles over, 186 -> 131 us; 8192 to 4608, 64 over,
-    // 288 -> 257; 8192 to 11264, 128 over, 647 -> 606).
+    // 288 -> 257; 8192 to 11264, 128 over, 647 -> 606).  Without full rounds, sums of
+    // 160 steps or more are all parts: 2048 to 2048 bf16, 64 tiles, 11264 long 117 us
+    // in smaller tiles, 111 in parts, 22528 long 220 and 180, but 8192 long 84 and 86,
+    // 4096 long 47 and 55; 2560 to 2048, 80 tiles, 11264 long 148 and 120.
     const int64_t tiles = (int64_t)a.mt * a.nt, rest = tiles % 256;
-    if (a.tile == WT && g.batches == 1 && tiles > 256 && rest > 0 && rest <= 128) {
+    if (a.tile == WT && g.batches == 1 && (tiles > 256 || all_parts) && rest > 0 && rest <= 128) {
         int64_t parts = 256 / rest;
         if (parts > steps / 8) parts = steps / 8;
         const double saved = steps * 1.6e-6 * (1.0 - 1.0 / (double)parts);
         const double cost = 2.0 * rest * parts * WT * WT * 4 / 4.5e12 + 5e-6;
-        if (parts >= 2 && saved > cost) {
+        if (parts >= 2 && (saved > cost || all_parts)) {
             a.tail_per = (int32_t)((steps + parts - 1) / parts);
             a.tail_splits = (int32_t)((steps + a.tail_per - 1) / a.tail_per);
             a.tail = (int32_t)rest;

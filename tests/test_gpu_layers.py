@@ -121,6 +121,24 @@ def test_tiles_left_over(dtype, rows, k, f):
 
 
 @pytest.mark.parametrize("dtype", [BF, HF])
+def test_all_tiles_in_parts(dtype):
+    """Long sums of too few tiles to fill the chip: every tile is made in parts, in the product and in its gradients."""
+    _check(40, dtype, None, 1544, 10248, 1800, "gelu", residual=True)
+    _check(41, dtype, None, 1544, 10248, 1032, "silu", gated=True)
+    _check(42, dtype, None, 1800, 1544, 10248, "tanh")
+    _check(43, dtype, None, 10248, 1544, 1800, "relu")
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("members,rows,k,f", [(None, 128, 520, 49160), (None, 136, 64, 49160), (None, 49160, 200, 128),
+                                              (200, 136, 136, 264), (200, 128, 72, 136)])
+def test_thin_products(dtype, members, rows, k, f):
+    """About as wide as one of the smaller tiles, and long."""
+    _check(44, dtype, members, rows, k, f, "silu", residual=True)
+    _check(45, dtype, members, rows, k, f // 2, "gelu", gated=True, bias=False)
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
 @pytest.mark.parametrize("members,rows,k,f,kw", [
     (None, 4100, 1031, 2051, {}), (None, 2049, 2052, 2047, {}), (3, 2050, 1031, 1029, {}), (3, 1401, 1031, 2051, dict(shared_w=True)),
     (3, 1401, 1031, 2051, dict(shared_x=True))])
