@@ -458,7 +458,8 @@ es_status es_gated_backward(const es_dense_grad_args* a, void* workspace, size_t
  *   are rounded.
  * p fp32; g of g_dtype; copy (NULL: none) receives p rounded to copy_dtype
  * (ES_BF16 or ES_F16).  lr and weight_decay are per tensor.  The tensors may
- * not overlap.  tensors: host array, read before the call returns. */
+ * not overlap.  tensors: host array, read before the call returns.  A call
+ * captured into a graph repeats its step number and rates at every replay. */
 typedef struct es_adamw_tensor {
     float* p;
     const void* g;

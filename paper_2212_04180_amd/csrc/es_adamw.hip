@@ -1,15 +1,16 @@
 // es_adamw.hip -- AdamW on many tensors in one launch, gfx950.
 //
 // Bound by memory: an element takes 28 bytes with 32-bit states and gradients
-// (16 and 1/8 with 8-bit states), against about 70 instructions.  One wave owns
+// (16 and 1/16 with 8-bit states), against about 70 instructions.  One wave owns
 // 256 consecutive elements, four a lane: the loads and stores of p, m, v are
 // 16 bytes a lane, and a block of 8-bit states that shares a scale is exactly
 // one wave's, so that its new scale is one reduction across the lanes and the
 // states are read and written once.
 //
 // Nothing is read twice, so the arrays go past the caches (nontemporal loads and
-// stores): 4096 x 11264 parameters with 32-bit states 1100 -> 989 us, with 8-bit
-// states 631 -> 580, one of 2^26 344 -> 304; of 2^22, which the caches hold, 21.1 -> 19.1.
+// stores): 2.06e8 parameters with 32-bit states, bf16 gradients and copies 1100 -> 989
+// us (5.8 TB/s), with 8-bit states and fp32 gradients 631 -> 580 (5.7 TB/s); 2^26 with 32-bit
+// states 344 -> 304, 2^22, which the caches hold, 21.1 -> 19.1.
 // Only where the last cache just holds a step's arrays (2^23 and 2^24 elements with
 // 32-bit states) steps that follow each other at once lose: 36.4 -> 38.8, 69.8 -> 75.3.
 #include <hip/hip_runtime.h>

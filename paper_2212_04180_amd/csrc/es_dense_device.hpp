@@ -295,7 +295,7 @@ __device__ __forceinline__ void wave_sync()
 // and a seventh of a 4096-long product's time.  lds: this wave's own.
 // STREAM: for launches whose outputs are more than the L2s hold (8 of 4 MB): stored
 // past them they leave the operands' rows there (8192 x 4096 -> 11264 bf16 with its
-// pre 711 -> 645 us).
+// pre 711 -> 640 us).
 // part: null, or where the sums of this wave's rows and columns go instead, rows
 // of 256, a gated layer's others 128 behind its gates.
 template <typename T, bool GATED, int MB, int NB, bool STREAM>

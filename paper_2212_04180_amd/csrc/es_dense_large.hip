@@ -416,7 +416,8 @@ __global__ __launch_bounds__(512, 2) void k_gemm_wide(GemmArgs a)
 }
 static_assert(8 * EPILOGUE_LDS<4> <= 4 * W_BYTES, "the epilogue's rows fit the buffers");
 
-// The tail's sums and their epilogue, four outputs a thread
+// The tail's sums and their epilogue, four outputs a thread.  Bound by memory: 67 MB of
+// sums of 64 tiles in 4 parts 12.6 us, 5.3 TB/s
 template <typename T, bool GATED>
 __global__ __launch_bounds__(256) void k_tail_join(GemmArgs a)
 {
@@ -509,7 +510,7 @@ bool large_fits(const Gemm& g)
 }
 
 // 256 x 256 tiles from 192 on (three quarters of the CUs: 4096 x 4096 -> 11264 bf16
-// 334 us against 390 in smaller ones).  With at most 128 of the smaller ones, a
+// 334 us against 390 in smaller ones), and where few of them have long sums (below).  With at most 128 of the smaller ones, a
 // long sum is split until the CUs have one each, 8 steps at least: a split's sums
 // pass through memory twice (1024^3 in 4 splits of 4 steps 25 us, in 2 of 8 21).
 void large_plan(GemmArgs& a)
