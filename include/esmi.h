@@ -422,7 +422,9 @@ typedef struct es_dense_args {
  * dx, dw, db: NULL to skip.  One whose member stride is 0 receives the sum
  * over the members (the gradient of an operand that they share).  All of the
  * type dtype; dz is rounded to it before the two products (db sums it
- * unrounded). */
+ * unrounded): by half a step of bf16 or fp16, and in ES_F16 a dz beyond 65,504
+ * is infinite and one below 2^-25 is 0, as dy itself would be (a program that
+ * meets either scales its loss). */
 typedef struct es_dense_grad_args {
     int32_t dtype, act;
     int64_t members, rows, in, out;
