@@ -29,12 +29,12 @@ __device__ __forceinline__ uintx4 piece(const T* row, int32_t k, int32_t K)
 {
     constexpr int E = 16 / sizeof(T);
     uintx4 v = {0, 0, 0, 0};
-    if (k + E <= K) {
+    if (K - k >= E) {  // (k + E may pass 2^31)
         __builtin_memcpy(&v, row + k, 16);
     } else if (k < K) {
         T t[E];
 #pragma unroll
-        for (int i = 0; i < E; ++i) t[i] = k + i < K ? row[k + i] : (T)0.f;
+        for (int i = 0; i < E; ++i) t[i] = i < K - k ? row[k + i] : (T)0.f;
         __builtin_memcpy(&v, t, 16);
     }
     return v;
