@@ -434,7 +434,10 @@ typedef struct es_dense_grad_args {
 /* workspace: device memory of at least the size that the _workspace query of
  * the same arguments gives (host value, no device work; 0: NULL is taken),
  * aligned to 256 bytes and used by this call alone until the stream has
- * passed it. */
+ * passed it.  A launch holds fewer than 2^32 work-items: members beyond that go
+ * in several, and where one member's product or gradient alone has more (2^30
+ * rows or outputs and above, with few columns) the call and its query return
+ * ES_ERR_UNSUPPORTED. */
 es_status es_dense_workspace(const es_dense_args* a, size_t* bytes);
 es_status es_dense(const es_dense_args* a, void* workspace, size_t bytes, void* hip_stream);
 es_status es_dense_backward_workspace(const es_dense_grad_args* a, size_t* bytes);

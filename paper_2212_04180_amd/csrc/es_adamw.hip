@@ -30,6 +30,9 @@ namespace {
 
 constexpr int MAX_TENSORS = 44;   // per launch: their table travels in the kernel's arguments
 constexpr int BLOCK = 256;        // elements that share a scale; one wave's work
+constexpr int LARGE_SPAN = 4;     // blocks of a wave of large calls
+// HIP takes fewer than 2^32 work-items a launch: a tensor's, in one launch
+constexpr int64_t MAX_GROUPS = 0xFFFFFFFFll / 256, MAX_N = MAX_GROUPS * 4 * LARGE_SPAN * BLOCK;
 constexpr float F8_MAX = 448.f;   // largest e4m3 value
 constexpr float F8_MIN = 0x1p-9f; // smallest above zero
 
@@ -251,7 +254,7 @@ bool aligned(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % 
 const char* tensor_bad(const es_adamw_args& a, const es_adamw_tensor& t)
 {
     const size_t ge = a.g_dtype == ES_F32 ? 4 : 2;
-    if (t.n < 0 || t.n > (int64_t)1 << 38) return "n is out of range";
+    if (t.n < 0 || t.n > MAX_N) return "n is out of range";
     if (!(t.lr >= 0.f) || !(t.lr < __builtin_inff())) return "lr must be finite and >= 0";
     if (!(t.weight_decay >= 0.f) || !(t.weight_decay < __builtin_inff())) return "weight_decay must be finite and >= 0";
     if (t.n == 0) return nullptr;
@@ -308,7 +311,7 @@ extern "C" es_status es_adamw(const es_adamw_args* a, const es_adamw_tensor* ten
     k.rbc1 = (float)(1.0 / (1.0 - std::pow((double)a->beta1, t)));
     k.rsbc2 = (float)(1.0 / std::sqrt(1.0 - std::pow((double)a->beta2, t)));
     k.eps = a->eps;
-    k.span = total > (int64_t)1 << 16 ? 4 : 1;
+    k.span = total > (int64_t)1 << 16 ? LARGE_SPAN : 1;
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
     for (int32_t i = 0; i < a->count;) {
         uint64_t grid = 0;
@@ -317,7 +320,7 @@ extern "C" es_status es_adamw(const es_adamw_args* a, const es_adamw_tensor* ten
             const es_adamw_tensor& x = tensors[i];
             if (x.n == 0) continue;
             const uint64_t groups = ((uint64_t)(x.n + BLOCK - 1) / BLOCK + 4 * k.span - 1) / (4 * k.span);
-            if (grid + groups > 0x7FFFFFFFu) break;  // at most 2^38 elements a tensor: never the first one
+            if (grid + groups > (uint64_t)MAX_GROUPS) break;  // at most MAX_N elements a tensor: never the first one
             const size_t ge = a->g_dtype == ES_F32 ? 16 : 8, se = a->state_bits == 32 ? 16 : 4;
             Tensor& d = k.t[k.count++];
             d = Tensor{x.p, x.g, x.m, x.v, x.m_scale, x.v_scale, x.copy, x.n, x.lr,

@@ -333,6 +333,8 @@ Packing packing(const Gemm& g)
     // any aligned address serves for the look
     if (p.a) p.a_bytes = pack_operand(h, true, reinterpret_cast<void*>(WORKSPACE_ALIGN));
     if (p.b) p.b_bytes = pack_operand(h, false, reinterpret_cast<void*>(WORKSPACE_ALIGN));
+    // (a copy of as many pieces as no launch holds is beyond any memory)
+    if (p.a_bytes / 16 + 256 > launch_groups(1) || p.b_bytes / 16 + 256 > launch_groups(1)) return Packing{};
     const double flops = 2.0 * g.batches * g.red * g.M * (g.gated ? 2.0 : 1.0) * g.N * g.K;
     const double gain = flops * (1 / 250e12 - 1 / 1100e12), cost = 2.0 * (p.a_bytes + p.b_bytes) / 4e12 + 4e-6 * (p.a + p.b);
     if (gain <= cost || !large_fits(h)) return Packing{};
@@ -352,7 +354,6 @@ hipError_t launch_pack(const Gemm& from, const Gemm& to, bool is_a, hipStream_t 
     a.batch = from.batches > 1 ? batch : red;
     a.row = is_a ? from.a_row : from.b_row;
     a.total = a.n * a.rows * (a.ld / 8);
-    if ((a.total + 255) / 256 > 0x7FFFFFFF) return hipErrorInvalidValue;  // beyond any memory
     k_pack<<<(unsigned)((a.total + 255) / 256), 256, 0, s>>>(a);
     return hipGetLastError();
 }
@@ -447,6 +448,31 @@ hipError_t launch_typed(const GemmArgs& a, hipStream_t s)
     if (g.gated) k_gemm_join<T, true><<<join, 256, 0, s>>>(a, total, quads, slices);
     else k_gemm_join<T, false><<<join, 256, 0, s>>>(a, total, quads, slices);
     return hipGetLastError();
+}
+
+int64_t threads_of(const GemmArgs& a)
+{
+    return a.path == PATH_ROWS ? 64 * a.mt : a.path == PATH_LARGE ? large_threads(a) : 256;
+}
+
+int64_t groups_per_batch(const GemmArgs& a)
+{
+    if (a.path == PATH_ROWS) return a.nt;
+    return (int64_t)a.splits * a.mt * a.nt + (a.tail ? (int64_t)a.tail * (a.tail_splits - 1) : 0);
+}
+
+// The product of the batches from b on
+Gemm from_batch(Gemm g, int64_t b)
+{
+    const int64_t e = (int64_t)dtype_size(g.dtype);
+    auto in = [&](const void* p, int64_t stride) -> const void* { return p ? static_cast<const char*>(p) + b * stride * e : p; };
+    g.a = in(g.a, g.a_batch);
+    g.b = in(g.b, g.b_batch);
+    g.bias = in(g.bias, g.bias_batch);
+    g.res = in(g.res, g.res_batch);
+    g.pre = const_cast<void*>(in(g.pre, g.pre_batch));
+    g.c = static_cast<char*>(g.c) + b * g.c_batch * (int64_t)dtype_size(g.c_dtype);
+    return g;
 }
 
 // ---- dz and its column sums -----------------------------------------------
@@ -585,10 +611,7 @@ bool gemm_too_large(const Gemm& g)
 {
     size_t n = 0;
     const GemmArgs a = plan(g, reinterpret_cast<void*>(WORKSPACE_ALIGN), &n);
-    const __int128 most = 0x7FFFFFFF;
-    if (a.path == PATH_ROWS) return (__int128)g.batches * a.nt > most;
-    return (__int128)g.batches * a.splits * a.mt * a.nt > most ||
-           (a.splits > 1 && (__int128)g.batches * g.M * join_quads(g) / 256 >= most);
+    return groups_per_batch(a) > launch_groups(threads_of(a));
 }
 
 hipError_t launch_gemm(const Gemm& g, void* workspace, size_t bytes, hipStream_t s)
@@ -599,58 +622,102 @@ hipError_t launch_gemm(const Gemm& g, void* workspace, size_t bytes, hipStream_t
     if (e != hipSuccess) return e;
     if (a.g.a != g.a) e = launch_pack(g, a.g, true, s);
     if (e == hipSuccess && a.g.b != g.b) e = launch_pack(g, a.g, false, s);
-    if (e != hipSuccess) return e;
-    switch (g.dtype) {
-    case ES_BF16: return launch_typed<__bf16>(a, s);
-    case ES_F16: return launch_typed<_Float16>(a, s);
-    default: return launch_typed<float>(a, s);
+    // as many batches as a launch holds (a split product has few tiles: one launch)
+    const int64_t most = launch_groups(threads_of(a)) / groups_per_batch(a);
+    for (int64_t b = 0; e == hipSuccess && b < a.g.batches; b += most) {
+        GemmArgs part = a;
+        part.g = from_batch(a.g, b);
+        part.g.batches = std::min(most, a.g.batches - b);
+        switch (g.dtype) {
+        case ES_BF16: e = launch_typed<__bf16>(part, s); break;
+        case ES_F16: e = launch_typed<_Float16>(part, s); break;
+        default: e = launch_typed<float>(part, s);
+        }
     }
+    return e;
 }
 
 int64_t gradz_chunks(int64_t rows) { return (rows + Z_ROWS - 1) / Z_ROWS; }
 
-__int128 gradz_workgroups(const GradZ& g)
+namespace {
+
+// Columns of workgroups, 2^lx threads side by side
+int64_t gradz_colblocks(const GradZ& g, int32_t* lx)
 {
     const int64_t pieces = ((int64_t)g.out * dtype_size(g.dtype) + 15) / 16;
-    int lx = 0;
-    while (lx < 5 && (int64_t)1 << lx < pieces) ++lx;
-    return (__int128)g.members * gradz_chunks(g.rows) * ((pieces + (1 << lx) - 1) >> lx);
+    *lx = 0;
+    while (*lx < 5 && (int64_t)1 << *lx < pieces) ++*lx;
+    return (pieces + (1 << *lx) - 1) >> *lx;
 }
+
+int64_t bias_colblocks(int64_t wide) { return (wide + 15) / 16; }
+
+unsigned bias_threads(int64_t count)
+{
+    unsigned threads = 64;
+    while (threads < 1024 && threads / 16 < count) threads *= 2;
+    return threads;
+}
+
+}  // namespace
+
+bool gradz_too_large(const GradZ& g)
+{
+    int32_t lx;
+    return (__int128)gradz_chunks(g.rows) * gradz_colblocks(g, &lx) > launch_groups(256);
+}
+
+bool bias_grad_too_large(int64_t count, int64_t wide) { return bias_colblocks(wide) > launch_groups(bias_threads(count)); }
 
 hipError_t launch_gradz(const GradZ& g, hipStream_t s)
 {
     GradZArgs a{};
     a.g = g;
     a.chunks = gradz_chunks(g.rows);
-    const size_t e = dtype_size(g.dtype);
-    const int64_t pieces = ((int64_t)g.out * e + 15) / 16;
-    while (a.lx < 5 && (int64_t)1 << a.lx < pieces) ++a.lx;
-    a.colblocks = (uint32_t)((pieces + (1 << a.lx) - 1) >> a.lx);
-    const int64_t grid = g.members * a.chunks * a.colblocks;
-    if (grid == 0) return hipSuccess;
-    auto go = [&](auto kernel) { kernel<<<(unsigned)grid, 256, 0, s>>>(a); };
-    switch (g.dtype) {
-    case ES_BF16: g.gated ? go(k_gradz<__bf16, true>) : go(k_gradz<__bf16, false>); break;
-    case ES_F16: g.gated ? go(k_gradz<_Float16, true>) : go(k_gradz<_Float16, false>); break;
-    default: g.gated ? go(k_gradz<float, true>) : go(k_gradz<float, false>);
+    a.colblocks = (uint32_t)gradz_colblocks(g, &a.lx);
+    const int64_t each = a.chunks * a.colblocks, e = (int64_t)dtype_size(g.dtype), wide = (g.gated ? 2 : 1) * (int64_t)g.out;
+    if (each == 0) return hipSuccess;
+    const int64_t most = launch_groups(256) / each;
+    for (int64_t n = 0; n < g.members; n += most) {
+        const int64_t count = std::min(most, g.members - n);
+        a.g.dy = static_cast<const char*>(g.dy) + n * g.dy_member * e;
+        if (g.pre) a.g.pre = static_cast<const char*>(g.pre) + n * g.pre_member * e;
+        if (g.dz) a.g.dz = static_cast<char*>(g.dz) + n * g.rows * g.ldz * e;
+        if (g.sums) a.g.sums = g.sums + n * a.chunks * wide;
+        if (g.db) a.g.db = static_cast<char*>(g.db) + n * g.db_member * e;
+        auto go = [&](auto kernel) { kernel<<<(unsigned)(count * each), 256, 0, s>>>(a); };
+        switch (g.dtype) {
+        case ES_BF16: g.gated ? go(k_gradz<__bf16, true>) : go(k_gradz<__bf16, false>); break;
+        case ES_F16: g.gated ? go(k_gradz<_Float16, true>) : go(k_gradz<_Float16, false>); break;
+        default: g.gated ? go(k_gradz<float, true>) : go(k_gradz<float, false>);
+        }
+        const hipError_t err = hipGetLastError();
+        if (err != hipSuccess) return err;
     }
-    return hipGetLastError();
+    return hipSuccess;
 }
 
 hipError_t launch_bias_grad(int32_t dtype, const float* sums, int64_t groups, int64_t count, int64_t wide, void* db,
                             int64_t db_member, hipStream_t s)
 {
-    const uint32_t colblocks = (uint32_t)((wide + 15) / 16);
-    unsigned threads = 64;
-    while (threads < 1024 && threads / 16 < count) threads *= 2;
-    const unsigned grid = (unsigned)(groups * colblocks);
-    auto go = [&](auto* out) { k_bias_grad<<<grid, threads, 0, s>>>(sums, count, wide, out, db_member, colblocks); };
-    switch (dtype) {
-    case ES_BF16: go(static_cast<__bf16*>(db)); break;
-    case ES_F16: go(static_cast<_Float16*>(db)); break;
-    default: go(static_cast<float*>(db));
+    const uint32_t colblocks = (uint32_t)bias_colblocks(wide);
+    const unsigned threads = bias_threads(count);
+    const int64_t most = launch_groups(threads) / colblocks;
+    for (int64_t n = 0; n < groups; n += most) {
+        const float* from = sums + n * count * wide;
+        const unsigned grid = (unsigned)(std::min(most, groups - n) * colblocks);
+        auto go = [&](auto* out) {
+            k_bias_grad<<<grid, threads, 0, s>>>(from, count, wide, out + n * db_member, db_member, colblocks);
+        };
+        switch (dtype) {
+        case ES_BF16: go(static_cast<__bf16*>(db)); break;
+        case ES_F16: go(static_cast<_Float16*>(db)); break;
+        default: go(static_cast<float*>(db));
+        }
+        const hipError_t err = hipGetLastError();
+        if (err != hipSuccess) return err;
     }
-    return hipGetLastError();
+    return hipSuccess;
 }
 
 }  // namespace esmi

@@ -12,6 +12,9 @@ namespace esmi {
 constexpr size_t WORKSPACE_ALIGN = 256;
 constexpr size_t workspace_up(size_t n) { return (n + WORKSPACE_ALIGN - 1) / WORKSPACE_ALIGN * WORKSPACE_ALIGN; }
 constexpr size_t dtype_size(int32_t t) { return t == ES_F32 ? 4 : 2; }
+// Workgroups of a launch at most: HIP takes fewer than 2^32 work-items.  What has
+// more goes in several launches of whole members; one member's work must fit.
+constexpr int64_t launch_groups(int64_t threads) { return 0xFFFFFFFFll / threads; }
 
 // One matrix product per batch, C[m][n] = sum over r < red and k < K of
 // A(m, k) B(n, k), and what follows it.  An operand is "k-major" where its k
@@ -47,7 +50,7 @@ struct Gemm {
 size_t gemm_workspace(const Gemm& g);
 // hipErrorInvalidValue where `bytes` is less than gemm_workspace gives
 hipError_t launch_gemm(const Gemm& g, void* workspace, size_t bytes, hipStream_t s);
-bool gemm_too_large(const Gemm& g);  // more workgroups than a launch holds
+bool gemm_too_large(const Gemm& g);  // one member's product has more workgroups than a launch holds
 
 // dz = dy act'(pre) (or both halves of a gated layer) in the type, rows of
 // ldz elements, and the column sums of the unrounded dz per chunk of rows.
@@ -65,9 +68,10 @@ struct GradZ {
     int64_t db_member;
 };
 int64_t gradz_chunks(int64_t rows);
-__int128 gradz_workgroups(const GradZ& g);
+bool gradz_too_large(const GradZ& g);
 hipError_t launch_gradz(const GradZ& g, hipStream_t s);
 // db[n][o], n < groups, from [groups][count][wide] sums
+bool bias_grad_too_large(int64_t count, int64_t wide);
 hipError_t launch_bias_grad(int32_t dtype, const float* sums, int64_t groups, int64_t count, int64_t wide, void* db,
                             int64_t db_member, hipStream_t s);
 

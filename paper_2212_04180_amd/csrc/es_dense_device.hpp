@@ -349,6 +349,7 @@ hipError_t launch_rows(const GemmArgs& a, hipStream_t s);
 bool large_takes(const Gemm& g, bool is_a);
 bool large_fits(const Gemm& g);
 void large_plan(GemmArgs& a);
+int64_t large_threads(const GemmArgs& a);  // of a workgroup
 hipError_t launch_large(const GemmArgs& a, hipStream_t s);
 
 }  // namespace esmi

@@ -458,7 +458,7 @@ hipError_t launch_kernel(const GemmArgs& a, hipStream_t s)
     const int bytes = wide ? 4 * W_BYTES : (deep ? 4 : 2) * 2 * M_BYTES;
     hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (e != hipSuccess) return e;
-    kernel<<<grid, wide ? 512 : 256, bytes, s>>>(a);
+    kernel<<<grid, (unsigned)large_threads(a), bytes, s>>>(a);
     e = hipGetLastError();
     if (e == hipSuccess && a.tail) {
         k_tail_join<T, GATED><<<(unsigned)a.tail * (WT * WT / (GATED ? 2 : 1) / 1024), 256, 0, s>>>(a);
@@ -559,6 +559,8 @@ void large_plan(GemmArgs& a)
         }
     }
 }
+
+int64_t large_threads(const GemmArgs& a) { return a.tile == WT ? 512 : 256; }
 
 hipError_t launch_large(const GemmArgs& a, hipStream_t s)
 {

@@ -15,6 +15,8 @@ using namespace esmi;
 namespace {
 
 constexpr int64_t kMaxDim = 0x7FFFFFFF;
+// Rows of all members taken as one product: as many as any launch holds (2^23 tiles of 128)
+constexpr int64_t kMaxMerged = 1 << 30;
 constexpr size_t kAlign = WORKSPACE_ALIGN;
 
 size_t up(size_t n) { return workspace_up(n); }
@@ -101,7 +103,7 @@ Gemm forward_gemm(const es_dense_args& a, bool gated)
     g.c = a.y.p; g.c_batch = a.y.member; g.c_row = a.y.row; g.c_dtype = a.y_dtype;
     // one network on all members' rows is one product where the rows follow each other
     const int64_t B = a.rows, n = a.members;
-    if (n > 1 && B * n <= kMaxDim && a.w.member == 0 && (!a.bias.p || a.bias.member == 0) && a.x.member == B * a.x.row &&
+    if (n > 1 && B * n <= kMaxMerged && a.w.member == 0 && (!a.bias.p || a.bias.member == 0) && a.x.member == B * a.x.row &&
         a.y.member == B * a.y.row && (!a.residual.p || a.residual.member == B * a.residual.row) &&
         (!a.pre.p || a.pre.member == B * a.pre.row)) {
         g.M = (int32_t)(B * n);
@@ -197,7 +199,7 @@ BackwardPlan plan_backward(const es_dense_grad_args& a, bool gated)
         p.dx.batches = 1; p.dx.red = n; p.dx.a_red = z_member; p.dx.b_red = a.w.member;
     } else {
         p.dx.batches = n; p.dx.red = 1; p.dx.a_batch = z_member; p.dx.b_batch = a.w.member;
-        if (n > 1 && B * n <= kMaxDim && a.w.member == 0 && z_member == B * z_row && a.dx.member == B * a.dx.row) {
+        if (n > 1 && B * n <= kMaxMerged && a.w.member == 0 && z_member == B * z_row && a.dx.member == B * a.dx.row) {
             p.dx.M = (int32_t)(B * n);
             p.dx.batches = 1;
         }
@@ -231,8 +233,10 @@ es_status backward(const es_dense_grad_args* a, bool gated, const char* who, voi
     Check c{who, a->members, a->rows};
     if (backward_bad(*a, gated, c)) return refuse(c);
     BackwardPlan p = plan_backward(*a, gated);
+    const bool sum_db = a->members != 1 && a->db.member == 0;
+    const int64_t db_count = sum_db ? a->members * p.chunks : p.chunks;
     if ((p.do_dx && gemm_too_large(p.dx)) || (p.do_dw && gemm_too_large(p.dw)) ||
-        gradz_workgroups(p.z) > kMaxDim || (__int128)a->members * ((p.wide + 15) / 16) > kMaxDim)
+        ((p.store_dz || p.do_db) && gradz_too_large(p.z)) || (p.do_db && !p.db_there && bias_grad_too_large(db_count, p.wide)))
         return init_fail(ES_ERR_UNSUPPORTED, "more workgroups than a launch holds", who);
     const size_t want = p.total();
     if (need) {
@@ -257,9 +261,7 @@ es_status backward(const es_dense_grad_args* a, bool gated, const char* who, voi
         if (p.store_dz) p.dx.a = p.dw.a = at;
     }
     if (e == hipSuccess && p.do_db && !p.db_there) {
-        const bool sum = a->members != 1 && a->db.member == 0;
-        e = launch_bias_grad(a->dtype, sums, sum ? 1 : a->members, sum ? a->members * p.chunks : p.chunks, p.wide, a->db.p,
-                             a->db.member, s);
+        e = launch_bias_grad(a->dtype, sums, sum_db ? 1 : a->members, db_count, p.wide, a->db.p, a->db.member, s);
     }
     if (e == hipSuccess && p.do_dx) e = launch_gemm(p.dx, partial, p.partial_bytes, s);
     if (e == hipSuccess && p.do_dw) e = launch_gemm(p.dw, partial, p.partial_bytes, s);

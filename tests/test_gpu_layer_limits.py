@@ -24,3 +24,39 @@ def test_longest_rows(dtype, k):
     assert y.item() == 36.0
     del x, w
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_more_members_than_a_launch_holds(dtype):
+    """2^24 + 5 members of one row: small whole numbers, so that every sum is exact."""
+    P = _P()
+    n = (1 << 24) + 5
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x, w, b, dy = (torch.randint(-3, 4, s, generator=g, device="cuda").to(dtype) for s in ((n, 1, 2), (n, 1, 2), (n, 1), (n, 1, 1)))
+    y, pre = P.dense(x, w, b, act="relu", keep_pre=True)
+    z = (x * w).sum(-1, keepdim=True) + b.unsqueeze(-1)
+    assert torch.equal(pre, z) and torch.equal(y, z.clamp_min(0))
+    dx, dw, db = P.dense_backward(dy, x, w, pre, act="relu")
+    dz = dy * (z > 0)
+    assert torch.equal(dx, dz * w) and torch.equal(dw, dz * x) and torch.equal(db, dz[:, 0])
+    # one network: sums over the members
+    y = P.dense(x, w[0], b[0], act="none")
+    assert torch.equal(y, (x * w[0]).sum(-1, keepdim=True) + b[0])
+    _, dw, db = P.dense_backward(dy, x, w[0], needs=(False, True, True))
+    # whole numbers below 2^24 are exact in any order; the result is rounded once
+    assert torch.equal(dw, (dy.double() * x.double()).sum(0).to(dtype)) and torch.equal(db, dy.double().sum((0, 1)).to(dtype))
+
+
+def test_more_bias_gradients_than_a_launch_holds():
+    """2^26 + 3 members of 65 rows: two chunks of rows each, added up by one workgroup a member."""
+    P = _P()
+    n = (1 << 26) + 3
+    dy = torch.zeros(n, 65, 1, dtype=torch.bfloat16, device="cuda")
+    a, b = (torch.arange(n, device="cuda") % p for p in (5, 7))
+    dy[:, 0, 0], dy[:, 64, 0] = a.to(dy.dtype), b.to(dy.dtype)
+    x = torch.zeros(65, 1, dtype=dy.dtype, device="cuda")
+    w = torch.zeros(1, 1, 1, dtype=dy.dtype, device="cuda").expand(n, 1, 1)
+    db = P.dense_backward(dy, x, w, needs=(False, False, True))[2]
+    assert torch.equal(db[:, 0], (a + b).to(dy.dtype))
+    del dy
+    torch.cuda.empty_cache()
