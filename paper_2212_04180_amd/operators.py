@@ -12,6 +12,7 @@ of their own.
 from __future__ import annotations
 
 import ctypes
+import math
 import struct
 
 import torch
@@ -110,6 +111,41 @@ def _first(t):
     return t.dtype, t.get_device()
 
 
+def _overlap(a, b):
+    """Whether matrices (of members) may share memory.  False only where they do not: their ranges are apart, or they
+    lie between each other's members or rows, which then repeat at common multiples."""
+    if a.numel() == 0 or b.numel() == 0:
+        return False
+    first = [t.data_ptr() for t in (a, b)]
+    steps = [[(n - 1, s * t.element_size()) for n, s in zip(t.shape, t.stride())] for t in (a, b)]
+
+    def span(dims, t):  # bytes from the first element of these dimensions to behind the last
+        return sum(n * s for n, s in dims) + t.element_size()
+
+    d = first[1] - first[0]
+    if d >= span(steps[0], a) or -d >= span(steps[1], b):
+        return False
+    for inner in (1, 2):  # dimensions of a block: a row, a member's matrix
+        every = math.gcd(*(s for dims in steps for n, s in dims[:-inner] if n))
+        if every and d % every >= span(steps[0][-inner:], a) and d % every + span(steps[1][-inner:], b) <= every:
+            return False
+    return True
+
+
+def _apart(out, x, w, bias, residual):
+    """out receives results while the operands are still read: only the residual's own elements are read by who writes
+    them."""
+    for name, t in (("x", x), ("w", w), ("bias", bias.unsqueeze(-2) if bias is not None else None)):
+        if t is not None and _overlap(out, t):
+            raise ValueError(f"out shares memory with {name}")
+    if residual is None or (out.data_ptr() == residual.data_ptr() and out.dtype is residual.dtype and
+                            [(n, s) for n, s in zip(out.shape, out.stride()) if n > 1] ==
+                            [(n, s) for n, s in zip(residual.shape, residual.stride()) if n > 1]):
+        return
+    if _overlap(out, residual):
+        raise ValueError("out shares memory with the residual, but is not the residual itself")
+
+
 def _members(named):
     """The one count of members among operands, None: none has any."""
     n = None
@@ -154,6 +190,8 @@ def _forward(entry, gated, x, w, bias, residual, act, keep_pre, out_dtype, out):
     py, _, _, ny = _matrix("out", y, ydt, dev, rows, f)
     if ny != n:
         raise ValueError("out has members exactly where an operand has")
+    if out is not None:
+        _apart(out, x, w, bias, residual)
     pre, pp = None, _NONE
     if keep_pre:
         pre = torch.empty(_shape(n, rows, wide), dtype=dt, device=dev)
@@ -205,8 +243,8 @@ def dense(x, w, bias=None, residual=None, act="none", keep_pre=False, out_dtype=
     in fp32.  Any strides whose rows are contiguous.  act: none, relu, tanh,
     gelu (erf form) or silu.  Returns y ([members,] rows, out) in the type, or
     fp32 with out_dtype; with keep_pre also x w^T + bias, which the gradient
-    takes.  out: where y goes; may be the residual itself.  stream: None, the
-    current one."""
+    takes.  out: where y goes; may be the residual itself, but share memory with
+    nothing else.  stream: None, the current one."""
     return _on(stream, _forward, "es_dense", False, x, w, bias, residual, act, keep_pre, out_dtype, out)
 
 

@@ -1,0 +1,81 @@
+"""Outputs that share memory with what a layer still reads: the binding's own check (CPU), and its refusals (marked gpu)."""
+import random
+
+import pytest
+import torch
+
+from paper_2212_04180_amd import operators
+
+
+def _addresses(t):
+    e = t.element_size()
+    at = {t.data_ptr()} if t.numel() else set()
+    for n, s in zip(t.shape, t.stride()):
+        at = {a + i * s * e for a in at for i in range(n)}
+    return {a + j for a in at for j in range(e)}
+
+
+def test_overlap_is_never_missed():
+    """Against every byte of random views, of two types, with and without members."""
+    rng = random.Random(3)
+    buf = torch.zeros(400)
+    seen = [0, 0]
+    for _ in range(3000):
+        views = []
+        for _ in range(2):
+            base = buf if rng.random() < 0.7 else buf.view(torch.bfloat16)
+            dims = rng.choice((2, 3))
+            shape = [rng.randint(0 if rng.random() < 0.1 else 1, 4) for _ in range(dims)]
+            stride = [rng.choice((0, 1, 3, 4, 8, 12, 16, 24, 48)) for _ in range(dims - 1)] + [1]
+            views.append(base.as_strided(shape, stride, rng.randint(0, 60)))
+        shared = bool(_addresses(views[0]) & _addresses(views[1]))
+        for a, b in (views, views[::-1]):
+            said = operators._overlap(a, b)
+            assert said or not shared, (a.shape, a.stride(), b.shape, b.stride())
+        seen[shared] += said == shared
+    assert min(seen) > 300
+
+
+def test_views_side_by_side_are_apart():
+    o = operators._overlap
+    buf = torch.zeros(6, 40)
+    assert not o(buf[:, :16], buf[:, 16:40]) and not o(buf[:, 16:40], buf[:, :16])  # columns of one buffer
+    assert not o(buf[:3], buf[3:]) and not o(buf[::2], buf[1::2])  # rows of it
+    assert o(buf[:, :17], buf[:, 16:40]) and o(buf, buf) and o(buf[2:4], buf[3:5])
+    arena = torch.zeros(5, 100)  # members' own inputs and outputs behind each other
+    x, y = arena[:, 3:27].unflatten(1, (4, 6)), arena[:, 27:59].unflatten(1, (4, 8))
+    assert not o(x, y) and not o(y, x) and o(x, arena[:, 26:58].unflatten(1, (4, 8)))
+    rows = torch.zeros(4, 5, 14)  # members within the rows
+    assert not o(rows[..., :6].transpose(0, 1), rows[..., 6:].transpose(0, 1))
+    assert not o(torch.zeros(2, 3), torch.zeros(2, 3)) and not o(buf[:0], buf)
+
+
+@pytest.mark.gpu
+def test_out_within_the_operands_is_refused():
+    D, G = operators.dense, operators.gated
+    for dtype in (torch.float32, torch.bfloat16):
+        x = torch.randn(40, 32, device="cuda").to(dtype)
+        w = torch.randn(32, 32, device="cuda").to(dtype)
+        b = torch.zeros(32, device="cuda", dtype=dtype)
+        keep = x.clone(), w.clone()
+        with pytest.raises(ValueError, match="shares memory with x"):
+            D(x, w, out=x)
+        with pytest.raises(ValueError, match="shares memory with w"):
+            D(x[:32], w, out=w)
+        with pytest.raises(ValueError, match="shares memory with bias"):
+            D(x[:1], w, b, out=b.view(1, 32))
+        with pytest.raises(ValueError, match="shares memory with x"):
+            G(x, w, out=x[:, :16])
+        buf = torch.zeros(41, 32, device="cuda", dtype=dtype)
+        with pytest.raises(ValueError, match="not the residual itself"):
+            D(x, w, residual=buf[:40], out=buf[1:])
+        with pytest.raises(ValueError, match="not the residual itself"):
+            D(x.expand(3, 40, 32), w, residual=buf[:40], out=buf[:40].expand(3, 40, 32))
+        assert torch.equal(x, keep[0]) and torch.equal(w, keep[1]) and not bool(buf.any())
+        # beside each other in one buffer, and the residual through another view of it
+        wide = torch.zeros(40, 64, device="cuda", dtype=dtype)
+        wide[:, :32] = x
+        assert torch.equal(D(wide[:, :32], w, out=wide[:, 32:]), D(x, w)) and torch.equal(wide[:, :32], x)
+        r = x.clone()
+        want = D(x, w, residual=x)
+        assert torch.equal(D(x, w, residual=r, out=r.view(40, 32)), want) and torch.equal(r, want)
