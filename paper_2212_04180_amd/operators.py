@@ -227,9 +227,18 @@ def _backward(entry, gated, dy, x, w, pre, act, needs):
     return dx, dw, db
 
 
-def _on(stream, f, *args):
+def _on(stream, tensors, f, *args):
+    """f on that stream.  It first waits for the current one, where the operands may still be being made, and they are
+    marked as in use there: a temporary freed on return is not handed out again before the kernels have passed."""
     if stream is None:
         return f(*args)
+    here = torch.cuda.current_stream(stream.device)
+    if stream == here:
+        return f(*args)
+    stream.wait_stream(here)
+    for t in tensors:
+        if t is not None and t.is_cuda:
+            t.record_stream(stream)
     with torch.cuda.stream(stream):
         return f(*args)
 
@@ -245,7 +254,7 @@ def dense(x, w, bias=None, residual=None, act="none", keep_pre=False, out_dtype=
     fp32 with out_dtype; with keep_pre also x w^T + bias, which the gradient
     takes.  out: where y goes; may be the residual itself, but share memory with
     nothing else.  stream: None, the current one."""
-    return _on(stream, _forward, "es_dense", False, x, w, bias, residual, act, keep_pre, out_dtype, out)
+    return _on(stream, (x, w, bias, residual, out), _forward, "es_dense", False, x, w, bias, residual, act, keep_pre, out_dtype, out)
 
 
 def dense_backward(dy, x, w, pre=None, act="none", needs=(True, True, True), stream=None):
@@ -254,7 +263,7 @@ def dense_backward(dy, x, w, pre=None, act="none", needs=(True, True, True), str
     members receives the sum over them.  needs: which to compute, None for the
     others.  dz = dy act'(pre) takes the type's precision and range before the
     products dx = dz w and dw = dz^T x; db sums it unrounded."""
-    return _on(stream, _backward, "es_dense_backward", False, dy, x, w, pre, act, needs)
+    return _on(stream, (dy, x, w, pre), _backward, "es_dense_backward", False, dy, x, w, pre, act, needs)
 
 
 def gated(x, w, bias=None, act="silu", keep_pre=False, out_dtype=None, out=None, stream=None):
@@ -262,12 +271,12 @@ def gated(x, w, bias=None, act="silu", keep_pre=False, out_dtype=None, out=None,
     first.  The first half of a gated feed-forward block; the second is
     dense(h, w_down, residual=x).  Shapes, types and strides as in dense; pre
     is [g, u], ([members,] rows, 2 out)."""
-    return _on(stream, _forward, "es_gated", True, x, w, bias, None, act, keep_pre, out_dtype, out)
+    return _on(stream, (x, w, bias, out), _forward, "es_gated", True, x, w, bias, None, act, keep_pre, out_dtype, out)
 
 
 def gated_backward(dh, x, w, pre, act="silu", needs=(True, True, True), stream=None):
     """(dx, dw, db) of gated for dh = dL/dh; see dense_backward."""
-    return _on(stream, _backward, "es_gated_backward", True, dh, x, w, pre, act, needs)
+    return _on(stream, (dh, x, w, pre), _backward, "es_gated_backward", True, dh, x, w, pre, act, needs)
 
 
 def adamw_state(params, bits=32):
@@ -304,10 +313,10 @@ def adamw(params, grads, m, v, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, weigh
     codes, one fp32 scale per 256 elements.  copies: bf16 or fp16 tensors that
     receive the new parameters.  lr, weight_decay: numbers, or one per tensor.
     All contiguous, none overlapping another.  A captured call repeats its
-    step number."""
+    step number.  stream: as in dense."""
     if stream is not None:
-        with torch.cuda.stream(stream):
-            return adamw(params, grads, m, v, step, lr, beta1, beta2, eps, weight_decay, m_scale, v_scale, copies)
+        tensors = [t for ts in (params, grads, m, v, m_scale, v_scale, copies) if ts is not None for t in ts]
+        return _on(stream, tensors, adamw, params, grads, m, v, step, lr, beta1, beta2, eps, weight_decay, m_scale, v_scale, copies)
     n = len(params)
     if n == 0:
         return
