@@ -232,6 +232,9 @@ def _on(stream, tensors, f, *args):
     marked as in use there: a temporary freed on return is not handed out again before the kernels have passed."""
     if stream is None:
         return f(*args)
+    for t in tensors:
+        if t is not None and t.is_cuda and t.device != stream.device:
+            raise ValueError(f"the stream is on {stream.device}, an operand on {t.device}")
     here = torch.cuda.current_stream(stream.device)
     if stream == here:
         return f(*args)

@@ -1,5 +1,7 @@
-"""Outputs that share memory with what a layer still reads: the binding's own check (CPU), and its refusals (marked gpu)."""
+"""Outputs that share memory with what a layer still reads: the binding's own check (CPU), and its refusals (marked gpu); streams
+of another device."""
 import random
+from types import SimpleNamespace
 
 import pytest
 import torch
@@ -48,6 +50,15 @@ def test_views_side_by_side_are_apart():
     rows = torch.zeros(4, 5, 14)  # members within the rows
     assert not o(rows[..., :6].transpose(0, 1), rows[..., 6:].transpose(0, 1))
     assert not o(torch.zeros(2, 3), torch.zeros(2, 3)) and not o(buf[:0], buf)
+
+
+def test_a_stream_of_another_device_is_refused():
+    """Without it the kernels would run on the operands' device, on whichever stream is current there."""
+    stream = SimpleNamespace(device=torch.device("cuda", 1))
+    here, there = (SimpleNamespace(is_cuda=True, device=torch.device("cuda", i)) for i in (0, 1))
+    for tensors in ([here], [there, None, here]):
+        with pytest.raises(ValueError, match="stream is on cuda:1, an operand on cuda:0"):
+            operators._on(stream, tensors, lambda: pytest.fail("called"))
 
 
 @pytest.mark.gpu
