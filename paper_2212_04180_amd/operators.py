@@ -7,7 +7,8 @@ True), cast where it is to run in 16 bits -- or of one network, their gradients,
 and an optimiser step outside es_tell.  Argument marshalling only, as in
 esmi.py; outputs and workspaces come from torch's allocator on the stream that
 the kernels run on.  Nothing is recorded by autograd: the gradients are calls
-of their own.
+of their own, and where autograd records (outside torch.no_grad()) the layers
+refuse operands that require a gradient.
 """
 from __future__ import annotations
 
@@ -67,6 +68,8 @@ def _matrix(name, t, dtype, device, rows, cols):
     shape, stride = t.shape, t.stride()
     if t.dtype is not dtype or t.get_device() != device:
         _place(name, t, dtype, device)
+    if t.requires_grad and torch.is_grad_enabled():
+        _unrecorded(name)
     if len(shape) == 2:
         (r, c), (row, one), member, n = shape, stride, 0, None
     elif len(shape) == 3:
@@ -85,6 +88,8 @@ def _vector(name, t, dtype, device, n, members):
     shape = t.shape
     if t.dtype is not dtype or t.get_device() != device:
         _place(name, t, dtype, device)
+    if t.requires_grad and torch.is_grad_enabled():
+        _unrecorded(name)
     if len(shape) not in (1, 2):
         raise ValueError(f"{name} has {len(shape)} dimensions, not 1 or, with members, 2")
     if shape[-1] != n:
@@ -100,6 +105,11 @@ def _place(name, t, dtype, device):
     if t.get_device() != device:
         raise ValueError(f"{name} is on {t.device}, not on cuda:{device}")
     raise ValueError(f"{name} is {t.dtype}, not {dtype}")
+
+
+def _unrecorded(name):
+    raise ValueError(f"{name} requires a gradient, and autograd does not record this call: under torch.no_grad(), or "
+                     f"detached, with the gradient from the _backward call")
 
 
 def _first(t):
