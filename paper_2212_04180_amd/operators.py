@@ -17,6 +17,7 @@ import math
 import struct
 
 import torch
+from torch.autograd.graph import increment_version  # autograd then knows a tensor that it saved as changed
 
 from . import esmi
 from .esmi import EsError
@@ -189,18 +190,21 @@ def _forward(entry, gated, x, w, bias, residual, act, keep_pre, out_dtype, out):
     if residual is not None:
         pr, _, _, nr = _matrix("residual", residual, dt, dev, rows, f)
     n = _members((("x", nx), ("w", nw), ("residual", nr)))
-    y = out
-    if y is None:
-        y = torch.empty(_shape(n, rows, f), dtype=out_dtype or dt, device=dev)
-    elif out_dtype is not None and y.dtype is not out_dtype:
-        raise ValueError(f"the output is {y.dtype}, not {out_dtype}")
-    ydt = y.dtype
+    if out is None:
+        y, ydt = None, out_dtype or dt
+    else:
+        y, ydt = out, out.dtype
+        if out_dtype is not None and ydt is not out_dtype:
+            raise ValueError(f"the output is {ydt}, not {out_dtype}")
     if ydt is not dt and ydt is not torch.float32:
         raise ValueError(f"the output is {dt} or fp32, not {ydt}")
-    py, _, _, ny = _matrix("out", y, ydt, dev, rows, f)
-    if ny != n:
-        raise ValueError("out has members exactly where an operand has")
-    if out is not None:
+    if y is None:
+        y = torch.empty(_shape(n, rows, f), dtype=ydt, device=dev)
+        py = y.data_ptr(), rows * f, f
+    else:
+        py, _, _, ny = _matrix("out", y, ydt, dev, rows, f)
+        if ny != n:
+            raise ValueError("out has members exactly where an operand has")
         _apart(out, x, w, bias, residual)
     pre, pp = None, _NONE
     if keep_pre:
@@ -209,6 +213,8 @@ def _forward(entry, gated, x, w, bias, residual, act, keep_pre, out_dtype, out):
     packed = _FORWARD.pack(_DTYPES[dt], _DTYPES[ydt], _act(act), 0, 1 if n is None else n, rows, k, f,
                            *px, *pw, *pb, *pr, *py, *pp)
     _launch(entry, packed, dev)
+    if out is not None:
+        increment_version(out)
     return (y, pre) if keep_pre else y
 
 
@@ -375,3 +381,4 @@ def adamw(params, grads, m, v, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, weigh
     table = struct.pack("=" + _TENSOR * n, *(e for row in zip(*cols) for e in row))
     head = _ADAMW.pack(n, _DTYPES[gdt], bits, _DTYPES[cdt], int(step), beta1, beta2, eps, 0)
     _check(esmi.lib().es_adamw(head, table, _stream(device)))
+    increment_version([*params, *m, *v, *(copies or ()), *(m_scale or ()), *(v_scale or ())])

@@ -68,3 +68,40 @@ def test_within_a_function_of_the_users_own():
     for a, w in zip(args, want):
         # sums of at most 24 terms of size 1, some ten roundings each way
         assert (a.grad - w).abs().max().item() <= 64 * 2.0 ** -24 * 24
+
+
+@pytest.mark.gpu
+def test_changed_tensors_are_known_as_changed():
+    """Autograd refuses to go back through a tensor that it saved and an operator has overwritten since."""
+    D = operators.dense
+    x, w = torch.randn(5, 8, device="cuda"), torch.randn(6, 8, device="cuda")
+    a = torch.randn(5, 6, device="cuda", requires_grad=True)
+    saved = a.exp()  # its gradient is itself
+    with torch.no_grad():
+        D(x, w, out=saved)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        saved.sum().backward()
+    saved = a.exp()
+    with torch.no_grad():
+        D(x, w, residual=saved, out=saved)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        saved.sum().backward()
+
+    p = [torch.randn(n, device="cuda", requires_grad=True) for n in (300, 7)]
+    for bits in (32, 8):
+        s = operators.adamw_state(p, bits)
+        g = [torch.randn_like(t) for t in p]
+        copies = [torch.zeros(t.shape, device="cuda", dtype=torch.bfloat16) for t in p]
+        before = {k: [t._version for t in ts] for k, ts in (("p", p), ("copies", copies), ("g", g), *s.items())}
+        loss = (p[0] * p[0].detach().clone().requires_grad_()).sum()
+        operators.adamw(p, g, s["m"], s["v"], 1, lr=0.1, m_scale=s.get("m_scale"), v_scale=s.get("v_scale"), copies=copies)
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            loss.backward()
+        for k, ts in (("p", p), ("copies", copies), *s.items()):
+            assert all(t._version > v for t, v in zip(ts, before[k])), (bits, k)
+        assert [t._version for t in g] == before["g"]
+    with torch.inference_mode():  # tensors without a version
+        q = [torch.randn(9, device="cuda")]
+        s = operators.adamw_state(q)
+        operators.adamw(q, [torch.ones(9, device="cuda")], s["m"], s["v"], 1, lr=0.1)
+        D(x, w, out=torch.empty(5, 6, device="cuda"))
