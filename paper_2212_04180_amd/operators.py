@@ -15,6 +15,7 @@ from __future__ import annotations
 import ctypes
 import math
 import struct
+from itertools import chain
 
 import torch
 from torch.autograd.graph import increment_version  # autograd then knows a tensor that it saved as changed
@@ -323,6 +324,22 @@ def _tensors(name, ts, n, dtype, device, sizes):
     return [t.data_ptr() for t in ts]
 
 
+def _distinct(cols, sizes, bits, copied):
+    """What is written is written for one tensor only, and is no gradient."""
+    lists = [0, 2, 3] + ([4, 5] if bits == 8 else []) + ([6] if copied else [])
+    flat = list(chain.from_iterable(cols[i] for i in lists))
+    seen = set(flat)
+    if len(seen) == len(flat) and seen.isdisjoint(cols[1]):
+        return
+    # empty tensors may lie anywhere
+    flat = [p for i in lists for p, k in zip(cols[i], sizes) if k]
+    seen = set(flat)
+    if len(seen) != len(flat):
+        raise ValueError("a parameter, state, scale or copy is listed twice")
+    if not seen.isdisjoint(p for p, k in zip(cols[1], sizes) if k):
+        raise ValueError("a gradient is also a parameter, state, scale or copy")
+
+
 def adamw(params, grads, m, v, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, m_scale=None, v_scale=None,
           copies=None, stream=None):
     """One AdamW step (step >= 1) on lists of tensors, in place, in few launches.
@@ -356,8 +373,6 @@ def adamw(params, grads, m, v, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, weigh
     bits = 32 if sdt is torch.float32 else 8
     cols = [_tensors("params", params, n, torch.float32, device, sizes), _tensors("grads", grads, n, gdt, device, sizes),
             _tensors("m", m, n, sdt, device, sizes), _tensors("v", v, n, sdt, device, sizes)]
-    if len(set(cols[0])) != n and len({p for p, k in zip(cols[0], sizes) if k}) != sum(k > 0 for k in sizes):
-        raise ValueError("a parameter is listed twice")
     if bits == 8:
         if m_scale is None or v_scale is None:
             raise ValueError("8-bit states need m_scale and v_scale")
@@ -378,7 +393,8 @@ def adamw(params, grads, m, v, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, weigh
         if len(each) != n:
             raise ValueError(f"{name}: one number, or one per parameter")
         cols.append(each)
-    table = struct.pack("=" + _TENSOR * n, *(e for row in zip(*cols) for e in row))
+    _distinct(cols, sizes, bits, copies is not None)
+    table = struct.pack("=" + _TENSOR * n, *chain.from_iterable(zip(*cols)))
     head = _ADAMW.pack(n, _DTYPES[gdt], bits, _DTYPES[cdt], int(step), beta1, beta2, eps, 0)
     _check(esmi.lib().es_adamw(head, table, _stream(device)))
     increment_version([*params, *m, *v, *(copies or ()), *(m_scale or ()), *(v_scale or ())])

@@ -90,3 +90,38 @@ def test_out_within_the_operands_is_refused():
         r = x.clone()
         want = D(x, w, residual=x)
         assert torch.equal(D(x, w, residual=r, out=r.view(40, 32)), want) and torch.equal(r, want)
+
+
+def test_adamw_tensors_listed_twice():
+    """Pointers as adamw gathers them: params, grads, m, v, scales, copies."""
+    ok = [[10, 20], [30, 40], [50, 60], [70, 80], [0, 0], [0, 0], [0, 0]]
+    operators._distinct(ok, [5, 6], 32, False)
+    operators._distinct([*ok[:6], [90, 100]], [5, 6], 32, True)
+    operators._distinct([*ok[:4], [110, 120], [130, 140], [90, 100]], [5, 6], 8, True)
+    operators._distinct([ok[0], [30, 30], *ok[2:]], [5, 6], 32, False)  # one gradient for two is only read
+    operators._distinct([[0, 20], [0, 40], [0, 60], [0, 80], *ok[4:]], [0, 6], 32, False)  # empty tensors
+    operators._distinct([[20, 20], [20, 40], *ok[2:]], [0, 6], 32, False)
+    for at, value in ((2, [50, 50]), (3, [50, 80]), (2, [10, 60]), (3, [70, 20])):
+        cols = [*ok[:at], value, *ok[at + 1:]]
+        with pytest.raises(ValueError, match="listed twice"):
+            operators._distinct(cols, [5, 6], 32, False)
+    for at, value in ((4, [110, 110]), (5, [130, 110]), (6, [90, 70]), (6, [10, 90])):
+        cols = [*ok[:4], [110, 120], [130, 140], [90, 100]]
+        cols[at] = value
+        with pytest.raises(ValueError, match="listed twice"):
+            operators._distinct(cols, [5, 6], 8, True)
+    for grads in ([10, 40], [30, 60], [80, 40]):
+        with pytest.raises(ValueError, match="a gradient is also"):
+            operators._distinct([ok[0], grads, *ok[2:]], [5, 6], 32, False)
+
+
+@pytest.mark.gpu
+def test_adamw_refuses_shared_states():
+    p, g, m, v = ([torch.ones(9, device="cuda") for _ in range(2)] for _ in range(4))
+    for call, word in ((lambda: operators.adamw(p, g, [m[0], m[0]], v, 1, lr=0.1), "twice"), (lambda: operators.adamw(p, g, m, m, 1, lr=0.1), "twice"),
+                       (lambda: operators.adamw(p, p, m, v, 1, lr=0.1), "gradient is also"), (lambda: operators.adamw([p[0], p[0]], g, m, v, 1, lr=0.1), "twice")):
+        with pytest.raises(ValueError, match=word):
+            call()
+    assert all(bool((t == 1).all()) for ts in (p, g, m, v) for t in ts)
+    operators.adamw(p, [g[0], g[0]], m, v, 1, lr=0.1)
+    assert torch.equal(p[0], p[1])
