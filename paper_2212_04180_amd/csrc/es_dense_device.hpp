@@ -31,6 +31,17 @@ __device__ __forceinline__ float act_tanh(float z)
     return s < 0.0625f ? near : far;
 }
 
+// Its slope 4 e / (1 + e)^2 with e = e^(-2|z|), which keeps its digits where tanh is
+// next to 1 ((1 - t) (1 + t) is off by 6e-2 at 8 and 0 at 10).
+template <bool FAST>
+__device__ __forceinline__ float tanh_slope(float z)
+{
+    const float a = __builtin_fabsf(z);
+    const float e = FAST ? __builtin_amdgcn_exp2f(a * (-2.f * LOG2E)) : expf(-2.f * a);
+    const float r = FAST ? __builtin_amdgcn_rcpf(1.f + e) : 1.f / (1.f + e);
+    return 4.f * e * (r * r);
+}
+
 // Phi(z), the normal distribution function.  FAST: Phi(-|z|) e^(z^2/2), which falls
 // slowly, as a polynomial without constant term in t = 1 / (1 + p |z|) (the form of
 // Abramowitz and Stegun 7.1.26), fitted here for the least relative error, 9e-8 for
@@ -82,8 +93,8 @@ __device__ __forceinline__ void activate(int32_t act, float z[W], float d[W])
     case ES_ACT_TANH:
 #pragma unroll
         for (int i = 0; i < W; ++i) {
+            if constexpr (SLOPE) d[i] = tanh_slope<FAST>(z[i]);
             z[i] = act_tanh<FAST>(z[i]);
-            if constexpr (SLOPE) d[i] = (1.f - z[i]) * (1.f + z[i]);
         }
         break;
     case ES_ACT_GELU:
