@@ -460,7 +460,7 @@ es_status es_gated_backward(const es_dense_grad_args* a, void* workspace, size_t
  *   2^-126): value = code * scale.  Codes are rounded to nearest; a sqrt(v)
  *   above 0 never becomes 0; a non-finite value is kept as NaN and leaves its
  *   neighbours' scale alone.  The step itself uses the moments before they
- *   are rounded.
+ *   are rounded; an eps between 0 and 2^-126 counts as 2^-126.
  * p fp32; g of g_dtype; copy (NULL: none) receives p rounded to copy_dtype
  * (ES_BF16 or ES_F16).  lr and weight_decay are per tensor.  The tensors may
  * not overlap.  tensors: host array, read before the call returns.  A call

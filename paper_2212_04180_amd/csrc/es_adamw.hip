@@ -310,7 +310,8 @@ extern "C" es_status es_adamw(const es_adamw_args* a, const es_adamw_tensor* ten
     k.bc2 = (float)(1.0 - std::pow((double)a->beta2, t));
     k.rbc1 = (float)(1.0 / (1.0 - std::pow((double)a->beta1, t)));
     k.rsbc2 = (float)(1.0 / std::sqrt(1.0 - std::pow((double)a->beta2, t)));
-    k.eps = a->eps;
+    // the 8-bit step multiplies by 1 / (root + eps), which for a root of 0 must be finite
+    k.eps = a->state_bits == 8 && a->eps > 0.f ? std::fmax(a->eps, 0x1p-126f) : a->eps;
     k.span = total > (int64_t)1 << 16 ? LARGE_SPAN : 1;
     hipStream_t s = static_cast<hipStream_t>(hip_stream);
     for (int32_t i = 0; i < a->count;) {
