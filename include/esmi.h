@@ -418,7 +418,8 @@ typedef struct es_dense_args {
  * activation: pre is not used and may be NULL):
  *   dz = dy act'(pre), or [dy u act'(g), dy act(g)] for gated;
  *   dx[n,i,k] = sum_o dz[n,i,o] w[n,o,k],  dw[n,o,k] = sum_i dz[n,i,o] x[n,i,k],
- *   db[n,o] = sum_i dz[n,i,o].  The residual's gradient is dy itself.
+ *   db[n,o] = sum_i dz[n,i,o].  The residual's gradient is dy itself (its sum over
+ *   the members where they share the residual).
  * dx, dw, db: NULL to skip.  One whose member stride is 0 receives the sum
  * over the members (the gradient of an operand that they share).  All of the
  * type dtype; dz is rounded to it before the two products (db sums it

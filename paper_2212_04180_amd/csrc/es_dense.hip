@@ -212,7 +212,7 @@ __global__ __launch_bounds__(256) void k_gemm(GemmArgs a)
 
 // Sums of the splits and the epilogue, four outputs a thread.  Few outputs leave
 // the chip idle: `slices` threads then share one's splits, each in its order.
-// Bound by memory, or its latency: 13 MB of sums of 250 x 131 outputs 6.6 us.
+// Bound by memory, or its latency: 11.3 MB of sums of 250 x 131 outputs (86 splits) 6.6 us.
 template <typename T, bool GATED>
 __global__ __launch_bounds__(256) void k_gemm_join(GemmArgs a, int64_t total, uint32_t quads, int32_t slices)
 {

@@ -278,11 +278,12 @@ def dense(x, w, bias=None, residual=None, act="none", keep_pre=False, out_dtype=
 
 
 def dense_backward(dy, x, w, pre=None, act="none", needs=(True, True, True), stream=None):
-    """(dx, dw, db) of dense for dy = dL/dy (the residual's gradient is dy),
-    shaped like x, w and the bias: an operand without members in a call with
-    members receives the sum over them.  needs: which to compute, None for the
-    others.  dz = dy act'(pre) takes the type's precision and range before the
-    products dx = dz w and dw = dz^T x; db sums it unrounded."""
+    """(dx, dw, db) of dense for dy = dL/dy (the residual's gradient is dy, or
+    dy.sum(0) where the members share it), shaped like x, w and the bias: an
+    operand without members in a call with members receives the sum over them.
+    needs: which to compute, None for the others.  dz = dy act'(pre) takes the
+    type's precision and range before the products dx = dz w and dw = dz^T x;
+    db sums it unrounded."""
     return _on(stream, (dy, x, w, pre), _backward, "es_dense_backward", False, dy, x, w, pre, act, needs)
 
 
