@@ -29,12 +29,13 @@ __device__ __forceinline__ uintx4 piece(const T* row, int32_t k, int32_t K)
 {
     constexpr int E = 16 / sizeof(T);
     uintx4 v = {0, 0, 0, 0};
-    if (K - k >= E) {  // (k + E may pass 2^31)
-        __builtin_memcpy(&v, row + k, 16);
-    } else if (k < K) {
+    const uint32_t at = (uint32_t)k, end = (uint32_t)K;  // at + E may pass 2^31
+    if (at + E <= end) {
+        __builtin_memcpy(&v, row + at, 16);
+    } else if (at < end) {
         T t[E];
 #pragma unroll
-        for (int i = 0; i < E; ++i) t[i] = i < K - k ? row[k + i] : (T)0.f;
+        for (int i = 0; i < E; ++i) t[i] = at + i < end ? row[at + i] : (T)0.f;
         __builtin_memcpy(&v, t, 16);
     }
     return v;
