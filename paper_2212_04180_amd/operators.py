@@ -48,7 +48,8 @@ def _launch(name, packed, device):
             return _launch(name, packed, device)
     lib, stream = esmi.lib(), _stream(device)
     rc = getattr(lib, name)(packed, None, 0, stream)
-    if rc == esmi.ES_OK:
+    if rc != esmi.ES_ERR_ARG:  # done, or failed with something perhaps enqueued
+        _check(rc)
         return
     n = ctypes.c_size_t(0)
     _check(getattr(lib, name + "_workspace")(packed, ctypes.byref(n)))
