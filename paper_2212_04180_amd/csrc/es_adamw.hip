@@ -19,6 +19,7 @@
 #include <cstdio>
 
 #include "es_internal.hpp"
+#include "es_launch.hpp"
 #include "esmi.h"
 
 // products and sums round by themselves unless written as one fma
@@ -227,9 +228,7 @@ __global__ __launch_bounds__(256) void k_adamw(AdamwArgs a)
 template <typename G, typename C>
 hipError_t launch_bits(int32_t bits, const AdamwArgs& k, unsigned grid, hipStream_t s)
 {
-    if (bits == 32) k_adamw<G, C, 32><<<grid, 256, 0, s>>>(k);
-    else k_adamw<G, C, 8><<<grid, 256, 0, s>>>(k);
-    return hipGetLastError();
+    return launch(bits == 32 ? k_adamw<G, C, 32> : k_adamw<G, C, 8>, grid, 256, 0, s, k);
 }
 
 template <typename G>
@@ -239,7 +238,7 @@ hipError_t launch_copy(const es_adamw_args& a, const AdamwArgs& k, unsigned grid
                                   : launch_bits<G, __bf16>(a.state_bits, k, grid, s);
 }
 
-hipError_t launch(const es_adamw_args& a, const AdamwArgs& k, unsigned grid, hipStream_t s)
+hipError_t launch_types(const es_adamw_args& a, const AdamwArgs& k, unsigned grid, hipStream_t s)
 {
     switch (a.g_dtype) {
     case ES_BF16: return launch_copy<__bf16>(a, k, grid, s);
@@ -330,7 +329,7 @@ extern "C" es_status es_adamw(const es_adamw_args* a, const es_adamw_tensor* ten
             grid += groups;
         }
         if (k.count == 0) break;
-        const hipError_t e = launch(*a, k, (unsigned)grid, s);
+        const hipError_t e = launch_types(*a, k, (unsigned)grid, s);
         if (e != hipSuccess) return init_fail(ES_ERR_HIP, hipGetErrorString(e), who);
     }
     return ES_OK;

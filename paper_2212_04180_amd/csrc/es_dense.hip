@@ -354,8 +354,7 @@ hipError_t launch_pack(const Gemm& from, const Gemm& to, bool is_a, hipStream_t 
     a.batch = from.batches > 1 ? batch : red;
     a.row = is_a ? from.a_row : from.b_row;
     a.total = a.n * a.rows * (a.ld / 8);
-    k_pack<<<(unsigned)((a.total + 255) / 256), 256, 0, s>>>(a);
-    return hipGetLastError();
+    return launch(k_pack, (unsigned)((a.total + 255) / 256), 256, 0, s, a);
 }
 
 bool odd(const Gemm& g, const void* p, int64_t row, int64_t batch, int64_t red)
@@ -410,19 +409,17 @@ GemmArgs plan(const Gemm& from, void* workspace, size_t* bytes)
 }
 
 template <typename T, int TM, int TN>
-void launch_staged(const GemmArgs& a, unsigned grid, hipStream_t s)
+hipError_t launch_staged(const GemmArgs& a, unsigned grid, hipStream_t s)
 {
     const Gemm& g = a.g;
+    void (*kernel)(GemmArgs) = nullptr;
     if (g.a_kmajor && g.b_kmajor) {
-        if constexpr (TM >= 64) {  // fewer rows have kernels of their own (es_dense_rows.hip)
-            if (g.gated) k_gemm<T, true, true, true, TM, TN><<<grid, 256, 0, s>>>(a);
-            else k_gemm<T, true, true, false, TM, TN><<<grid, 256, 0, s>>>(a);
-        }
-    } else if (g.a_kmajor) {
-        k_gemm<T, true, false, false, TM, TN><<<grid, 256, 0, s>>>(a);
+        if constexpr (TM >= 64)  // fewer rows have kernels of their own (es_dense_rows.hip)
+            kernel = g.gated ? k_gemm<T, true, true, true, TM, TN> : k_gemm<T, true, true, false, TM, TN>;
     } else {
-        k_gemm<T, false, false, false, TM, TN><<<grid, 256, 0, s>>>(a);
+        kernel = g.a_kmajor ? k_gemm<T, true, false, false, TM, TN> : k_gemm<T, false, false, false, TM, TN>;
     }
+    return kernel ? launch(kernel, grid, 256, 0, s, a) : hipErrorInvalidValue;
 }
 
 uint32_t join_quads(const Gemm& g) { return (uint32_t)(((int64_t)g.N + 3) / 4); }
@@ -435,19 +432,16 @@ hipError_t launch_typed(const GemmArgs& a, hipStream_t s)
     const unsigned grid = (unsigned)(g.batches * a.splits * a.mt * a.nt);
     hipError_t e = hipSuccess;
     if (a.path == PATH_LARGE) e = launch_large(a, s);
-    else if (a.tile == 128) launch_staged<T, 128, 128>(a, grid, s);
-    else if (a.tile == 64) launch_staged<T, 64, 64>(a, grid, s);
-    else launch_staged<T, 32, 128>(a, grid, s);
-    if (e == hipSuccess) e = hipGetLastError();
+    else if (a.tile == 128) e = launch_staged<T, 128, 128>(a, grid, s);
+    else if (a.tile == 64) e = launch_staged<T, 64, 64>(a, grid, s);
+    else e = launch_staged<T, 32, 128>(a, grid, s);
     if (e != hipSuccess || a.splits == 1) return e;
     const uint32_t quads = join_quads(g);
     const int64_t total = g.batches * g.M * quads;
     int32_t slices = 1;
     while (slices < 16 && slices * 4 <= a.splits && total * slices < 131072) slices *= 2;
     const unsigned join = (unsigned)((total * slices + 255) / 256);
-    if (g.gated) k_gemm_join<T, true><<<join, 256, 0, s>>>(a, total, quads, slices);
-    else k_gemm_join<T, false><<<join, 256, 0, s>>>(a, total, quads, slices);
-    return hipGetLastError();
+    return launch(g.gated ? k_gemm_join<T, true> : k_gemm_join<T, false>, join, 256, 0, s, a, total, quads, slices);
 }
 
 int64_t threads_of(const GemmArgs& a)
@@ -685,13 +679,13 @@ hipError_t launch_gradz(const GradZ& g, hipStream_t s)
         if (g.dz) a.g.dz = static_cast<char*>(g.dz) + n * g.rows * g.ldz * e;
         if (g.sums) a.g.sums = g.sums + n * a.chunks * wide;
         if (g.db) a.g.db = static_cast<char*>(g.db) + n * g.db_member * e;
-        auto go = [&](auto kernel) { kernel<<<(unsigned)(count * each), 256, 0, s>>>(a); };
+        void (*kernel)(GradZArgs);
         switch (g.dtype) {
-        case ES_BF16: g.gated ? go(k_gradz<__bf16, true>) : go(k_gradz<__bf16, false>); break;
-        case ES_F16: g.gated ? go(k_gradz<_Float16, true>) : go(k_gradz<_Float16, false>); break;
-        default: g.gated ? go(k_gradz<float, true>) : go(k_gradz<float, false>);
+        case ES_BF16: kernel = g.gated ? k_gradz<__bf16, true> : k_gradz<__bf16, false>; break;
+        case ES_F16: kernel = g.gated ? k_gradz<_Float16, true> : k_gradz<_Float16, false>; break;
+        default: kernel = g.gated ? k_gradz<float, true> : k_gradz<float, false>;
         }
-        const hipError_t err = hipGetLastError();
+        const hipError_t err = launch(kernel, (unsigned)(count * each), 256, 0, s, a);
         if (err != hipSuccess) return err;
     }
     return hipSuccess;
@@ -706,15 +700,15 @@ hipError_t launch_bias_grad(int32_t dtype, const float* sums, int64_t groups, in
     for (int64_t n = 0; n < groups; n += most) {
         const float* from = sums + n * count * wide;
         const unsigned grid = (unsigned)(std::min(most, groups - n) * colblocks);
-        auto go = [&](auto* out) {
-            k_bias_grad<<<grid, threads, 0, s>>>(from, count, wide, out + n * db_member, db_member, colblocks);
+        hipError_t err;
+        auto go = [&](auto kernel, auto* out) {
+            err = launch(kernel, grid, threads, 0, s, from, count, wide, out + n * db_member, db_member, colblocks);
         };
         switch (dtype) {
-        case ES_BF16: go(static_cast<__bf16*>(db)); break;
-        case ES_F16: go(static_cast<_Float16*>(db)); break;
-        default: go(static_cast<float*>(db));
+        case ES_BF16: go(k_bias_grad<__bf16>, static_cast<__bf16*>(db)); break;
+        case ES_F16: go(k_bias_grad<_Float16>, static_cast<_Float16*>(db)); break;
+        default: go(k_bias_grad<float>, static_cast<float*>(db));
         }
-        const hipError_t err = hipGetLastError();
         if (err != hipSuccess) return err;
     }
     return hipSuccess;

@@ -5,6 +5,7 @@
 #include <math.h>
 
 #include "es_dense.hpp"
+#include "es_launch.hpp"
 
 namespace esmi {
 

@@ -458,12 +458,8 @@ hipError_t launch_kernel(const GemmArgs& a, hipStream_t s)
     const int bytes = wide ? 4 * W_BYTES : (deep ? 4 : 2) * 2 * M_BYTES;
     hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (e != hipSuccess) return e;
-    kernel<<<grid, (unsigned)large_threads(a), bytes, s>>>(a);
-    e = hipGetLastError();
-    if (e == hipSuccess && a.tail) {
-        k_tail_join<T, GATED><<<(unsigned)a.tail * (WT * WT / (GATED ? 2 : 1) / 1024), 256, 0, s>>>(a);
-        e = hipGetLastError();
-    }
+    e = launch(kernel, grid, (unsigned)large_threads(a), (size_t)bytes, s, a);
+    if (e == hipSuccess && a.tail) e = launch(k_tail_join<T, GATED>, (unsigned)a.tail * (WT * WT / (GATED ? 2 : 1) / 1024), 256, 0, s, a);
     return e;
 }
 

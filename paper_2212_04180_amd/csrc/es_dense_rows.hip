@@ -158,10 +158,9 @@ __global__ __launch_bounds__(64 * MOST_WAVES) void k_rows(GemmArgs a)
 }
 
 template <typename T, bool GATED, bool ODD>
-void launch_rows_of(const GemmArgs& a, unsigned grid, unsigned threads, hipStream_t s)
+hipError_t launch_rows_of(const GemmArgs& a, unsigned grid, unsigned threads, hipStream_t s)
 {
-    if (a.g.M <= 16) k_rows<T, GATED, 1, ODD><<<grid, threads, 0, s>>>(a);
-    else k_rows<T, GATED, 2, ODD><<<grid, threads, 0, s>>>(a);
+    return launch(a.g.M <= 16 ? k_rows<T, GATED, 1, ODD> : k_rows<T, GATED, 2, ODD>, grid, threads, 0, s, a);
 }
 
 template <typename T>
@@ -170,14 +169,10 @@ hipError_t launch_typed(const GemmArgs& a, hipStream_t s)
     const unsigned grid = (unsigned)(a.g.batches * a.nt), threads = 64u * a.mt;
     if constexpr (sizeof(T) == 2) {
         if (a.odd_a || a.odd_b) {
-            if (a.g.gated) launch_rows_of<T, true, true>(a, grid, threads, s);
-            else launch_rows_of<T, false, true>(a, grid, threads, s);
-            return hipGetLastError();
+            return a.g.gated ? launch_rows_of<T, true, true>(a, grid, threads, s) : launch_rows_of<T, false, true>(a, grid, threads, s);
         }
     }
-    if (a.g.gated) launch_rows_of<T, true, false>(a, grid, threads, s);
-    else launch_rows_of<T, false, false>(a, grid, threads, s);
-    return hipGetLastError();
+    return a.g.gated ? launch_rows_of<T, true, false>(a, grid, threads, s) : launch_rows_of<T, false, false>(a, grid, threads, s);
 }
 
 }  // namespace
