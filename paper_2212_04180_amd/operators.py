@@ -399,4 +399,4 @@ def adamw(params, grads, m, v, step, lr, beta1=0.9, beta2=0.999, eps=1e-8, weigh
     table = struct.pack("=" + _TENSOR * n, *chain.from_iterable(zip(*cols)))
     head = _ADAMW.pack(n, _DTYPES[gdt], bits, _DTYPES[cdt], int(step), beta1, beta2, eps, 0)
     _check(esmi.lib().es_adamw(head, table, _stream(device)))
-    increment_version([*params, *m, *v, *(copies or ()), *(m_scale or ()), *(v_scale or ())])
+    increment_version([*params, *m, *v, *(t for ts in (copies, m_scale, v_scale) if ts is not None for t in ts)])

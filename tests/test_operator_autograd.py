@@ -105,3 +105,18 @@ def test_changed_tensors_are_known_as_changed():
         s = operators.adamw_state(q)
         operators.adamw(q, [torch.ones(9, device="cuda")], s["m"], s["v"], 1, lr=0.1)
         D(x, w, out=torch.empty(5, 6, device="cuda"))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("bits", [32, 8])
+def test_rows_of_one_tensor_as_the_lists(bits):
+    """Lists may be a tensor's rows, as well for copies and scales; all of it counts as changed."""
+    p, g = torch.zeros(3, 256, device="cuda"), torch.ones(3, 256, device="cuda")
+    s = operators.adamw_state(list(p), bits)
+    s = {k: torch.stack([t.view(torch.uint8) if t.dtype == torch.float8_e4m3fn else t for t in ts]) for k, ts in s.items()}
+    if bits == 8:
+        s["m"], s["v"] = (s[k].view(torch.float8_e4m3fn) for k in ("m", "v"))
+    copies = torch.zeros(3, 256, device="cuda", dtype=torch.bfloat16)
+    before = copies._version
+    operators.adamw(p, g, s["m"], s["v"], 1, lr=0.5, m_scale=s.get("m_scale"), v_scale=s.get("v_scale"), copies=copies)
+    assert bool(((p + 0.5).abs() < 1e-6).all()) and torch.equal(copies, p.bfloat16()) and copies._version > before
